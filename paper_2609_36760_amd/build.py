@@ -1,11 +1,11 @@
 """Build ``libmla_lowbit.so`` in-tree for gfx950.
 
 The HIP translation units are compiled by ``hipcc --offload-arch=gfx950``;
-the host ABI translation unit is plain C++ and is compiled by ``g++`` against
+the host ABI translation units are plain C++ and are compiled by ``g++`` against
 the HIP runtime headers only.  Flags that matter for results:
 
 * ``-fhip-fp32-correctly-rounded-divide-sqrt`` and ``-ffp-contract=off`` on
-  the writer: the quantizer's divisions and additions are single IEEE
+  the writers: the quantizer's divisions and additions are single IEEE
   roundings, so packed codes and fp16 metadata are bit-exact;
 * ``-fno-gpu-flush-denormals-to-zero``: fp16 subnormal scales survive;
 * ``-Xclang -target-feature -Xclang -packed-fp32-ops``: no packed fp32 ALU
@@ -40,6 +40,8 @@ HIP_FLAGS = [
 ]
 PER_FILE = {
     "quant_append.hip": ["-ffp-contract=off"],
+    "norm_rope_append.hip": ["-ffp-contract=off"],
+    "rope_queries.hip": ["-ffp-contract=off"],
 }
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__",
               "-I", os.path.join(ROCM, "include"), "-I", INCLUDE, "-I", CSRC]

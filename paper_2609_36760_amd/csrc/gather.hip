@@ -1,0 +1,166 @@
+// Cached tokens read back as dense bf16 rows (mla_*_gather): the packed codes of
+// a token become bf16(scale * (q - zero)), the product rounded to fp32 first;
+// BF16 rows (the BF16 cache, protected tokens) are copied bit for bit.
+//
+// A wave takes the 512 content channels of kRows output rows (64 lanes x 8
+// channels: one 4-bit code word in, 16 bytes out), or the RoPE keys of 8 rows.
+// The bytes written are three times the bytes read, so the work split follows
+// the output: every store instruction writes whole rows.
+#include <hip/hip_runtime.h>
+
+#include "internal.h"
+#include "kernel_common.h"
+#include "prefill_internal.h"
+
+namespace mla {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRopeRows = 8;        // of a RoPE wave
+
+// Sequence of output row r: how many of cu_rows[1 .. B] are at or below it
+// (r uniform in the wave; B at the rows behind the last sequence).
+__device__ __forceinline__ int sequence_of(const GatherArgs& a, int r, int lane) {
+    int b = 0;
+    for (int i = 0; i < a.B; i += 64) {
+        const int c = i + lane < a.B ? a.cu_rows[1 + i + lane] : INT32_MAX;
+        b += __popcll(__ballot(c <= r));
+    }
+    return b;
+}
+
+// Where a token is: a BF16 row, or offset `off` of a packed page.
+struct Source {
+    const uint8_t* row;     // null: packed
+    const uint8_t* page;
+    int off;
+};
+template <bool kBf16, bool kProt>
+__device__ __forceinline__ Source source_of(const GatherArgs& a, int b, int r) {
+    const int64_t pos = max(static_cast<int64_t>(a.first != nullptr ? a.first[b] : 0) + r - a.cu_rows[b], int64_t{0});
+    if constexpr (kProt) {
+        const int64_t L = a.seq_lens[b];
+        if (pos < L && (pos < a.sink || pos >= L - a.recent)) {      // (the second implies recent >= 1)
+            const int64_t ps = min(max(static_cast<int64_t>(a.prot_slot[b]), int64_t{0}), a.num_prot - 1);
+            const int64_t row = pos < a.sink ? pos : a.sink + (pos - a.sink) % a.recent;
+            return {a.prot + (ps * (a.sink + a.recent) + row) * 1152, nullptr, 0};
+        }
+    }
+    const int32_t p = static_cast<int32_t>(min(pos, static_cast<int64_t>(INT32_MAX)));
+    const int column = page_column(p, a.g.page_size, a.max_pages);
+    const int64_t id = min(max(static_cast<int64_t>(a.block_table[static_cast<int64_t>(b) * a.max_pages + column]), int64_t{0}),
+                           a.num_pages - 1);
+    const uint8_t* page = a.cache + id * a.g.page_bytes;
+    const int off = p % a.g.page_size;
+    if constexpr (kBf16) return {page + static_cast<int64_t>(off) * 1152, nullptr, 0};
+    return {nullptr, page, off};
+}
+
+// Eight channels of one group: codes of 4 bits (channel 2i of the word at bits
+// 4i, channel 2i + 1 in the upper half), or of 2 bits at `shift`.
+template <int BITS>
+__device__ __forceinline__ uint4 values(uint32_t word, int shift, float scale, float zero) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = (word >> (shift + BITS * i)) & ((1u << BITS) - 1), hi = (word >> (16 + shift + BITS * i)) & ((1u << BITS) - 1);
+        o[i] = kc::pack_bf16x2(scale * (static_cast<float>(lo) - zero), scale * (static_cast<float>(hi) - zero));
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ void fp16_meta(uint32_t w, float& scale, float& zero) {
+    scale = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w & 0xFFFFu)));
+    zero = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16)));
+}
+
+// Channels 8 lane .. of the content, or with `rope` channels 8 lig .. of the key.
+template <int CBITS, bool kPaper>
+__device__ __forceinline__ uint4 read(const GatherArgs& a, const Source& s, bool rope, int lane) {
+    const int column = rope ? 1024 + (lane & 7) * 16 : lane * 16;
+    if (CBITS == 16 || s.row != nullptr) return *reinterpret_cast<const uint4*>(s.row + column);
+    float scale, zero;
+    const uint8_t* rec = s.page + a.g.off_mc + static_cast<int64_t>(s.off) * 32;
+    if (rope) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(s.page + a.g.off_cr + s.off * 32 + (lane & 7) * 4);
+        if constexpr (kPaper) {
+            scale = *reinterpret_cast<const float*>(rec + 24);
+            zero = static_cast<float>(rec[28]);
+        } else {
+            fp16_meta(*reinterpret_cast<const uint32_t*>(s.page + a.g.off_mr + s.off * 4), scale, zero);
+        }
+        return values<4>(w, 0, scale, zero);
+    }
+    const int g = lane >> 3;
+    if constexpr (kPaper) {
+        scale = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(rec + 2 * g)) << 16);
+        zero = static_cast<float>(rec[16 + g]);
+    } else {
+        fp16_meta(*reinterpret_cast<const uint32_t*>(rec + 4 * g), scale, zero);
+    }
+    if constexpr (CBITS == 4)
+        return values<4>(*reinterpret_cast<const uint32_t*>(s.page + s.off * 256 + lane * 4), 0, scale, zero);
+    else
+        return values<2>(*reinterpret_cast<const uint32_t*>(s.page + s.off * 128 + (lane >> 1) * 4), 8 * (lane & 1), scale, zero);
+}
+
+// CBITS 16: the BF16 cache.
+template <int CBITS, bool kProt, bool kPaper, int kRows>
+__global__ __launch_bounds__(kThreads) void gather_kernel(GatherArgs a) {
+    const int lane = static_cast<int>(threadIdx.x & 63);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane((blockIdx.x * kThreads + threadIdx.x) >> 6);
+    const uint32_t content_waves = (static_cast<uint32_t>(a.n) + kRows - 1) / kRows;
+    if (wave < content_waves) {
+        const int first = static_cast<int>(wave) * kRows;
+        uint4 x[kRows];
+        bool there[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int b = sequence_of(a, first + i, lane);
+            there[i] = first + i < a.n && b < a.B;
+            if (there[i]) x[i] = read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, first + i), false, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (there[i]) *reinterpret_cast<uint4*>(a.c_out + static_cast<int64_t>(first + i) * a.c_out_stride + lane * 8) = x[i];
+        return;
+    }
+    const int first = static_cast<int>(wave - content_waves) * kRopeRows;
+    const int r = first + (lane >> 3);
+    int b = a.B;
+#pragma unroll
+    for (int i = 0; i < kRopeRows; ++i) {
+        const int bi = sequence_of(a, first + i, lane);
+        if ((lane >> 3) == i) b = bi;
+    }
+    if (r >= a.n || b >= a.B) return;
+    const uint4 x = read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, r), true, lane);
+    *reinterpret_cast<uint4*>(a.k_out + static_cast<int64_t>(r) * a.k_out_stride + (lane & 7) * 8) = x;
+}
+
+template <int CBITS, bool kProt, bool kPaper>
+hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
+    constexpr int kRows = 1;
+    const int64_t n = a.n;
+    const int64_t waves = (n + kRows - 1) / kRows + (n + kRopeRows - 1) / kRopeRows;
+    static_assert((kMaxAppendTokens + kMaxAppendTokens / kRopeRows + 1) * 64 + kThreads <= kMaxDispatchItems, "launch size");
+    const int64_t groups = (waves * 64 + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL((gather_kernel<CBITS, kProt, kPaper, kRows>), dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0,
+                       stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_gather(const GatherArgs& a, bool lowbit, hipStream_t stream) {
+    if (!lowbit) return launch_as<16, false, false>(a, stream);
+    const bool prot = a.prot != nullptr, paper = a.g.paper_meta != 0;
+    if (a.g.c_bits == 4) {
+        if (prot) return paper ? launch_as<4, true, true>(a, stream) : launch_as<4, true, false>(a, stream);
+        return paper ? launch_as<4, false, true>(a, stream) : launch_as<4, false, false>(a, stream);
+    }
+    if (prot) return paper ? launch_as<2, true, true>(a, stream) : launch_as<2, true, false>(a, stream);
+    return paper ? launch_as<2, false, true>(a, stream) : launch_as<2, false, false>(a, stream);
+}
+
+}  // namespace mla

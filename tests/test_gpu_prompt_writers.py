@@ -1,0 +1,402 @@
+"""The writers with norm and rotation, the readers and the queries' rotation (GPU).
+
+Dense rows equal the 64-bit formulas' bf16 values bit for bit, cache bytes the
+oracle's packing of those rows, protection rows the rows themselves; the
+readers give bf16(scale * (q - zero)) of the oracle's codes, and protected
+tokens bit for bit.
+"""
+import numpy as np
+import pytest
+
+from oracle import paged_cache as pc
+from oracle import protection as op
+from prefill_ref import bits, rms_norm, rotate, rotation_table
+
+pytestmark = pytest.mark.gpu
+
+POSITIONS = 3000
+EPS = 1e-6
+KINDS = [(4, "fp16"), (4, "paper"), (2, "fp16"), (2, "paper"), (16, "bf16")]
+
+
+class Batch:
+    """A paged cache, its table, and tokens [first, lens) of every sequence."""
+
+    def __init__(self, first, lens, kind, page=64, seed=0, prot=None):
+        import torch
+
+        from paper_2609_36760_amd import _binding as mb
+        from paper_2609_36760_amd import _prefill as mp
+        self.mb, self.mp = mb, mp
+        self.cbits, meta = kind
+        self.bf16, self.first, self.lens, self.page, self.prot_policy = self.cbits == 16, first, lens, page, prot
+        self.fmt = mb.cache_format(c_bits=4 if self.bf16 else self.cbits, page_size=page,
+                                   meta=mb.MLA_META_PAPER if meta == "paper" else mb.MLA_META_FP16)
+        self.ofmt = None if self.bf16 else pc.CacheFormat(c_bits=self.cbits, page_size=page, meta=meta)
+        rng = np.random.default_rng(seed)
+        counts = [max(1, -(-n // page)) for n in lens]
+        self.num_pages = sum(counts) + 2
+        ids = rng.permutation(self.num_pages)
+        self.table = np.zeros((len(lens), max(counts) + 1), np.int32)
+        at = 0
+        for b, k in enumerate(counts):
+            self.table[b, :k] = ids[at:at + k]
+            at += k
+        self.page_bytes = mb.mla_bf16_page_bytes(self.fmt) if self.bf16 else mb.mla_lowbit_page_bytes(self.fmt)
+        self.cache = torch.full((self.num_pages * self.page_bytes,), 0x5A, dtype=torch.uint8, device="cuda")
+        self.seq = np.concatenate([np.full(n - f, b, np.int32) for b, (f, n) in enumerate(zip(first, lens))])
+        self.pos = np.concatenate([np.arange(f, n, dtype=np.int32) for f, n in zip(first, lens)])
+        self.slots = self.table[self.seq, self.pos // page].astype(np.int64) * page + self.pos % page
+        self.n = len(self.seq)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed + 1)
+        gain = torch.ones(512, device="cuda")
+        gain[::97] = 12.0
+        self.x = (torch.randn((self.n, 512), generator=g, device="cuda") * gain).bfloat16()
+        self.k = (torch.randn((self.n, 64), generator=g, device="cuda") * 3.0).bfloat16()
+        self.w = (1.0 + 0.3 * torch.randn(512, generator=g, device="cuda")).bfloat16()
+        self.cu = np.concatenate([[0], np.cumsum([n - f for f, n in zip(first, lens)])]).astype(np.int32)
+        self.rotary = rotation_table(POSITIONS).cuda()
+        if prot is not None:
+            self.policy = mb.protect_policy(*prot)
+            self.num_prot = len(lens) + 1
+            self.prot_slot = rng.permutation(self.num_prot)[:len(lens)].astype(np.int32)
+            self.prot = torch.full((self.num_prot, sum(prot), 576), 3.0, device="cuda").bfloat16()
+
+    def dev(self, a):
+        import torch
+        return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+    def append(self, norm="weight", halves=False, dense=True, stream=None, x=None, k=None, in_place=False, slots=None):
+        import torch
+        x, k = self.x if x is None else x, self.k if k is None else k
+        nrm = None if norm is None else self.mp.rms_norm(EPS, self.w if norm == "weight" else None)
+        rot = self.mp.rotation(self.rotary, int(halves))
+        self.c_out = (x if in_place else torch.full((self.n, 520), 9.0, device="cuda").bfloat16()[:, :512]) if dense else None
+        self.k_out = (k if in_place else torch.full((self.n, 64), 9.0, device="cuda").bfloat16()) if dense else None
+        head = (nrm, rot, x, k, self.dev(self.pos), self.dev(self.slots if slots is None else slots), self.cache, self.num_pages)
+        tail = dict(c_out=self.c_out, k_out=self.k_out, stream=stream)
+        if self.prot_policy is not None:
+            self.mp.mla_lowbit_norm_rope_append_protected(
+                self.fmt, self.policy, *head, self.dev(self.seq), self.dev(np.asarray(self.lens, np.int32)),
+                self.dev(self.prot_slot), self.prot, self.num_prot, **tail)
+        elif self.bf16:
+            self.mp.mla_bf16_norm_rope_append(self.fmt, *head, **tail)
+        else:
+            self.mp.mla_lowbit_norm_rope_append(self.fmt, *head, **tail)
+
+    def want_rows(self, norm="weight", halves=False):
+        import torch
+        x, k, w = self.x.cpu(), self.k.cpu(), self.w.cpu()
+        c = x if norm is None else rms_norm(x, w if norm == "weight" else None, EPS)
+        rows = self.rotary.cpu()[torch.from_numpy(self.pos.astype(np.int64))]
+        return c, rotate(k, rows, halves)
+
+    def want_cache(self, c, k, slots):
+        want = np.full(self.num_pages * self.page_bytes, 0x5A, np.uint8)
+        if self.bf16:
+            rows = want.view(np.uint16).reshape(-1, 576)
+            keep = slots >= 0
+            rows[slots[keep]] = np.concatenate([bits(c), bits(k)], axis=1)[keep]
+        else:
+            pc.write_tokens(want, self.ofmt, slots, bits(c), bits(k))
+        return want
+
+    def want_prot(self, c, k, before):
+        want = bits(before).reshape(self.num_prot, -1, 576).copy()
+        for b, L in enumerate(self.lens):
+            m = self.seq == b
+            op.write_protection(want[self.prot_slot[b]], self.pos[m], L, bits(c)[m], bits(k)[m], *self.prot_policy)
+        return want
+
+    def gather(self, n=None, first=True, stream=None, cu=None):
+        import torch
+        n = self.n if n is None else n
+        self.c_read = torch.full((n, 528), 9.0, device="cuda").bfloat16()[:, :512]
+        self.k_read = torch.full((n, 64), 9.0, device="cuda").bfloat16()
+        f = self.dev(np.asarray(self.first, np.int32)) if first else None
+        head = (self.cache, self.num_pages, self.dev(self.table), self.dev(self.cu if cu is None else cu))
+        if self.prot_policy is not None:
+            self.mp.mla_lowbit_gather_protected(self.fmt, self.policy, *head, self.dev(np.asarray(self.lens, np.int32)),
+                                                self.prot, self.num_prot, self.dev(self.prot_slot), self.c_read, self.k_read,
+                                                f, stream=stream)
+        elif self.bf16:
+            self.mp.mla_bf16_gather(self.fmt, *head, self.c_read, self.k_read, f, stream=stream)
+        else:
+            self.mp.mla_lowbit_gather(self.fmt, *head, self.c_read, self.k_read, f, stream=stream)
+
+    def want_read(self, c, k):
+        """bf16 bits of the tokens' stored values."""
+        from oracle import quantizer as qz
+        if self.bf16:
+            return bits(c), bits(k)
+        ch, kh = pc.encode_sequence_dense(self.ofmt, bits(c), bits(k))      # fp32
+        # (f32_to_bf16 gives the bf16 value as fp32)
+        cb, kb = (np.ascontiguousarray(qz.f32_to_bf16(v)).view(np.uint32) >> 16 for v in (ch, kh))
+        cb, kb = cb.astype(np.uint16), kb.astype(np.uint16)
+        if self.prot_policy is not None:
+            for b, L in enumerate(self.lens):
+                held = (self.seq == b) & np.isin(self.pos, op.protected_positions(L, *self.prot_policy))
+                cb[held], kb[held] = bits(c)[held], bits(k)[held]
+        return cb, kb
+
+
+def equal_bits(got, want, what):
+    g = bits(got)
+    # (zeros of either sign are one value)
+    same = (g == want) | (((g | want) & 0x7FFF) == 0)
+    assert same.all(), f"{what}: {np.count_nonzero(~same)} of {same.size} values differ"
+
+
+SIZES = [([0], [1]), ([5], [14]), ([0, 130, 7, 63], [257, 131, 7, 130]), ([0] * 70, list(range(1, 71)))]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("first,lens", SIZES)
+@pytest.mark.parametrize("norm,halves", [("weight", False), ("plain", True), (None, False)])
+def test_append_and_read_back(kind, first, lens, norm, halves):
+    import torch
+    b = Batch(first, lens, kind, seed=len(lens))
+    b.append(norm, halves)
+    b.gather()
+    torch.cuda.synchronize()
+    c, k = b.want_rows(norm, halves)
+    equal_bits(b.c_out, bits(c), "normalized latents")
+    equal_bits(b.k_out, bits(k), "rotated keys")
+    got = b.cache.cpu().numpy()
+    assert np.array_equal(got, b.want_cache(c, k, b.slots)), "cache bytes differ from the oracle's packing"
+    cw, kw = b.want_read(c, k)
+    equal_bits(b.c_read, cw, "latents read back")
+    equal_bits(b.k_read, kw, "keys read back")
+
+
+@pytest.mark.parametrize("kind", KINDS[:4])
+@pytest.mark.parametrize("prot", [(4, 128), (0, 3), (7, 0), (1, 40)])
+@pytest.mark.parametrize("first,lens", [([0], [1]), ([0, 100, 3, 0], [300, 139, 4, 133]), ([131], [132])])
+def test_protected_append_and_read_back(kind, prot, first, lens):
+    import torch
+    b = Batch(first, lens, kind, seed=7, prot=prot)
+    before = b.prot.clone()
+    b.append("weight", False)
+    b.gather()
+    torch.cuda.synchronize()
+    c, k = b.want_rows("weight", False)
+    assert np.array_equal(b.cache.cpu().numpy(), b.want_cache(c, k, b.slots)), "cache bytes"
+    assert np.array_equal(bits(b.prot), b.want_prot(c, k, before)), "protection rows"
+    cw, kw = b.want_read(c, k)
+    equal_bits(b.c_read, cw, "latents read back")
+    equal_bits(b.k_read, kw, "keys read back")
+
+
+@pytest.mark.parametrize("page", [32, 96, 1024])
+@pytest.mark.parametrize("kind", [(4, "fp16"), (2, "paper"), (16, "bf16")])
+def test_page_sizes(page, kind):
+    import torch
+    b = Batch([3, 0], [200, 97], kind, page=page, seed=page)
+    b.append("plain", True)
+    b.gather()
+    torch.cuda.synchronize()
+    c, k = b.want_rows("plain", True)
+    assert np.array_equal(b.cache.cpu().numpy(), b.want_cache(c, k, b.slots))
+    cw, kw = b.want_read(c, k)
+    equal_bits(b.c_read, cw, "latents")
+    equal_bits(b.k_read, kw, "keys")
+
+
+@pytest.mark.parametrize("kind", [(4, "fp16"), (16, "bf16")])
+def test_padding_tokens_and_rows_behind_the_last_sequence(kind):
+    """A padded batch: tokens without a slot leave the cache alone (their dense rows are written), and rows behind
+    the last sequence stay as they were; positions of skipped tokens may be anything."""
+    import torch
+    b = Batch([0, 0], [50, 30], kind, seed=2)
+    slots, pos = b.slots.copy(), b.pos.copy()
+    skipped = np.arange(b.n) % 3 == 1
+    slots[skipped] = -1
+    slots[np.nonzero(skipped)[0][:3]] = [-(1 << 40), b.num_pages * b.page, 1 << 50]
+    wild = pos.copy()
+    wild[skipped] = np.resize(np.array([-1, 1 << 30, -(1 << 31), POSITIONS], np.int64), int(skipped.sum())).astype(np.int32)
+    b.pos = wild
+    b.append("weight", False, slots=slots)
+    b.pos = pos
+    torch.cuda.synchronize()
+    c, k = b.want_rows("weight", False)
+    slots[skipped] = -1
+    assert np.array_equal(b.cache.cpu().numpy(), b.want_cache(c, k, slots))
+    equal_bits(b.c_out, bits(c), "dense latents, skipped tokens included")
+    keep = torch.from_numpy(~skipped).cuda()
+    equal_bits(b.k_out[keep], bits(k)[~skipped], "dense keys")
+    b.append("weight", False)
+    b.gather(n=b.n + 9)
+    torch.cuda.synchronize()
+    cw, kw = b.want_read(c, k)
+    equal_bits(b.c_read[:b.n], cw, "latents")
+    assert bool((b.c_read[b.n:] == 9.0).all()) and bool((b.k_read[b.n:] == 9.0).all()), "rows behind the last sequence"
+
+
+def test_empty_ranges_and_no_first():
+    import torch
+    b = Batch([0, 0, 0], [40, 9, 70], (4, "fp16"), seed=4)
+    b.append()
+    torch.cuda.synchronize()
+    c, k = b.want_rows()
+    cu = np.array([0, 11, 11, 81], np.int32)            # 11 tokens of the first, none of the second, all of the third
+    b.gather(n=81, first=False, cu=cu)
+    torch.cuda.synchronize()
+    pick = np.concatenate([np.arange(11), 49 + np.arange(70)])
+    cw, kw = b.want_read(c, k)
+    equal_bits(b.c_read, cw[pick], "latents")
+    equal_bits(b.k_read, kw[pick], "keys")
+
+
+@pytest.mark.parametrize("halves", [False, True])
+def test_in_place_rows(halves):
+    import torch
+    b = Batch([0], [100], (4, "fp16"), seed=5)
+    c, k = b.want_rows("weight", halves)
+    b.append("weight", halves, in_place=True)
+    torch.cuda.synchronize()
+    equal_bits(b.x, bits(c), "in place latents")
+    equal_bits(b.k, bits(k), "in place keys")
+    assert np.array_equal(b.cache.cpu().numpy(), b.want_cache(c, k, b.slots))
+
+
+def test_strided_inputs_and_extreme_latents():
+    """Views of one projection's output; rows of zeros, of one value, of huge and of tiny values."""
+    import torch
+    b = Batch([0], [64], (4, "fp16"), seed=6)
+    x = b.x.clone()
+    x[0] = 0.0
+    x[1] = 3.0
+    x[2] *= 1e30
+    x[3] *= 1e-30
+    x[4] = 0.0
+    x[4, 77] = -2.0
+    x[5] = 2.0 ** -133
+    x[6] = 3.3e38
+    joint = torch.cat([x, b.k], dim=1)                  # [n, 576]
+    b.x, b.k = joint[:, :512], joint[:, 512:]
+    b.append("weight", False)
+    b.gather()
+    torch.cuda.synchronize()
+    c, k = b.want_rows("weight", False)
+    equal_bits(b.c_out, bits(c), "normalized latents")
+    assert np.array_equal(b.cache.cpu().numpy(), b.want_cache(c, k, b.slots))
+
+
+def test_large_prompt_equals_its_parts():
+    """One call over 4 000 tokens writes what calls over its parts write."""
+    import torch
+    whole, parts = (Batch([0, 0], [2900, 1100], (4, "fp16"), seed=8, prot=(4, 128)) for _ in range(2))
+    whole.append()
+    for a in range(0, parts.n, 700):
+        e = min(parts.n, a + 700)
+        parts.mp.mla_lowbit_norm_rope_append_protected(
+            parts.fmt, parts.policy, parts.mp.rms_norm(EPS, parts.w), parts.mp.rotation(parts.rotary), parts.x[a:e],
+            parts.k[a:e], parts.dev(parts.pos[a:e]), parts.dev(parts.slots[a:e]), parts.cache, parts.num_pages,
+            parts.dev(parts.seq[a:e]), parts.dev(np.asarray(parts.lens, np.int32)), parts.dev(parts.prot_slot), parts.prot,
+            parts.num_prot)
+    torch.cuda.synchronize()
+    assert torch.equal(whole.cache, parts.cache) and torch.equal(whole.prot, parts.prot)
+
+
+@pytest.mark.parametrize("n,H", [(1, 1), (3, 16), (77, 5), (1000, 128)])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("how", ["out", "in place", "heads"])
+def test_rope_queries(n, H, halves, how):
+    import torch
+
+    from paper_2609_36760_amd import _prefill as mp
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + H)
+    q = torch.randn((n, H, 192), generator=g, device="cuda").bfloat16()
+    pos = torch.randint(0, POSITIONS, (n,), generator=g, device="cuda").to(torch.int32)
+    pos[0] = POSITIONS - 1
+    table = rotation_table(POSITIONS).cuda()
+    want = rotate(q[..., 128:], table[pos.long()][:, None], halves)
+    before = q.clone()
+    view = q[..., 128:]
+    if how == "out":
+        out = torch.empty((n, H, 64), dtype=torch.bfloat16, device="cuda")
+    elif how == "in place":
+        out = view
+    else:
+        out = torch.empty((H, n, 72), dtype=torch.bfloat16, device="cuda").transpose(0, 1)[..., :64]
+    mp.mla_rope_queries(mp.rotation(table, int(halves)), view, pos, out)
+    torch.cuda.synchronize()
+    equal_bits(out.contiguous(), bits(want), "rotated queries")
+    assert torch.equal(q[..., :128], before[..., :128])
+    if how != "in place":
+        assert torch.equal(q, before)
+
+
+def test_streams_and_graphs():
+    """Append and read back captured and replayed, and on a side stream, equal the eager calls."""
+    import torch
+
+    from paper_2609_36760_amd import _prefill as mp
+    b = Batch([0, 20], [300, 90], (4, "fp16"), seed=10, prot=(4, 128))
+    args = [b.dev(a) for a in (b.pos, b.slots, b.seq, np.asarray(b.lens, np.int32), b.prot_slot, b.table, b.cu,
+                               np.asarray(b.first, np.int32))]
+    pos, slots, seq, lens, pslot, table, cu, first = args
+    norm, rot = mp.rms_norm(EPS, b.w), mp.rotation(b.rotary)
+    c, k, c2, k2 = (torch.zeros((b.n, w), dtype=torch.bfloat16, device="cuda") for w in (512, 64, 512, 64))
+    q = torch.randn((b.n, 4, 64), device="cuda").bfloat16()
+    q2 = torch.zeros_like(q)
+
+    def step(stream=None):
+        mp.mla_lowbit_norm_rope_append_protected(b.fmt, b.policy, norm, rot, b.x, b.k, pos, slots, b.cache, b.num_pages, seq,
+                                                 lens, pslot, b.prot, b.num_prot, c, k, stream=stream)
+        mp.mla_lowbit_gather_protected(b.fmt, b.policy, b.cache, b.num_pages, table, cu, lens, b.prot, b.num_prot, pslot, c2,
+                                       k2, first, stream=stream)
+        mp.mla_rope_queries(rot, q, pos, q2, stream=stream)
+
+    outs = (b.cache, b.prot, c, k, c2, k2, q2)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+
+    def poison():
+        for t in outs:
+            t.fill_(1)
+        torch.cuda.synchronize()
+
+    # (bytes that the step does not write were 0x5A / 3.0: compare what it writes)
+    start_cache, start_prot = torch.full_like(b.cache, 0x5A), torch.full_like(b.prot, 3.0)
+
+    def reset():
+        poison()
+        b.cache.copy_(start_cache)
+        b.prot.copy_(start_prot)
+        torch.cuda.synchronize()
+
+    reset()
+    step(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, want)), "side stream"
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for rep in range(3):
+        reset()
+        g.replay()
+        torch.randn(1 << 16, device="cuda").sin_()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), f"replay {rep}"
+
+
+def test_wrong_tensors_are_refused():
+    b = Batch([0], [10], (4, "fp16"))
+    rot, mp = b.mp.rotation(b.rotary), b.mp
+    good = [b.fmt, None, rot, b.x, b.k, b.dev(b.pos), b.dev(b.slots), b.cache, b.num_pages]
+    for at, bad in ((3, b.x[:5]), (3, b.x.float()), (3, b.x.half()), (4, b.k[:, :32]), (5, b.dev(b.slots)), (6, b.dev(b.pos)),
+                    (7, b.cache[:100]), (3, b.x.cpu()), (6, b.dev(b.slots)[:3])):
+        with pytest.raises(ValueError):
+            mp.mla_lowbit_norm_rope_append(*good[:at], bad, *good[at + 1:])
+    with pytest.raises(ValueError):
+        mp.rotation(b.rotary.double())
+    with pytest.raises(ValueError):
+        mp.rms_norm(1e-6, b.w[:100])
+    with pytest.raises(ValueError):
+        mp.mla_rope_queries(rot, b.x.reshape(10, 8, 64), b.dev(b.pos)[:4])
+    with pytest.raises(ValueError):
+        mp.mla_lowbit_gather(b.fmt, b.cache, b.num_pages, b.dev(b.table), b.dev(b.cu)[:1], b.x, b.k)
