@@ -11,8 +11,8 @@
 //      wave's 32 rows, K = 192 channels in 12 steps), Q^T in registers
 //      throughout: a lane ends up with one row's scores for half of the keys,
 //      its partner lane ^ 32 with the other half;
-//   3. one pass over the scores: running reference (lazily moved maximum),
-//      weights 2^(s - reference) in fp32, rounded to bf16, their sum;
+//   3. one pass over the scores: weights 2^(s - reference) in fp32 on the row's
+//      running reference, rounded to bf16, their sums;
 //   4. O^T[channel][row] += V^T . P^T (M = 128 channels in 4 blocks, K = KT
 //      keys): P^T comes straight from the score registers, because the
 //      transposing LDS reads fetch V's keys in the order in which the score
@@ -24,10 +24,13 @@
 // scaled by that key's rounding; lse takes the sum of the fp32 weights.
 // Scores, reference, sums and accumulators are fp32.
 //
-// The reference.  The weights stay below 2^kSlack: only when a row's maximum
-// passes its reference by more are the accumulators rescaled, which after the
-// first tiles is rare.  It starts at the lowest finite value, so that hidden
-// scores (-inf) weigh 0 without a test.
+// The reference.  bf16 has the range of fp32, so a row's weights may be taken on
+// any reference that keeps them far from overflow: a row's is its maximum over
+// its first tile, and it stays until a tile's weights add up to kMost or more
+// (or to no number); then it moves to that tile's maximum, the accumulators
+// follow, and the tile is weighed again.  So the maximum is only looked for in
+// such tiles.  The reference starts at the lowest finite value: hidden scores
+// (-inf) weigh 0 on it, every other overflows and moves it.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -44,7 +47,10 @@ using kc::f32x16;
 using kc::i16x4;
 using kc::lds_i16x4;
 
-constexpr float kSlack = 8.0f;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kMost = 0x1p30f;
 constexpr float kUnset = -FLT_MAX;
 
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
@@ -123,42 +129,62 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
 
     const int r = wave * kRowsPerWave + col;        // the lane's row of the block
     const int seen = static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + r));
-    // of the wave's rows that exist: the fewest and the most keys seen
+    const int see_first = static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0)));   // of row 0
+    // the most keys that a row of this wave sees (rows that exist)
     const int r_first = wave * kRowsPerWave, r_last = min(r_first + kRowsPerWave, q_rows) - 1;
-    const int see_min = static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + r_first));
     const int see_max = r_last < r_first ? key0
                                          : static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + r_last));
 
     // ---- staging ----------------------------------------------------------
-    const uint8_t* const kn = reinterpret_cast<const uint8_t*>(a.k_nope.data + static_cast<int64_t>(kv_row) * a.k_nope.stride_t +
-                                                                static_cast<int64_t>(head) * a.k_nope.stride_h);
-    const uint8_t* const kr = reinterpret_cast<const uint8_t*>(a.k_rope.data + static_cast<int64_t>(kv_row) * a.k_rope.stride_t);
-    const uint8_t* const vv = reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(kv_row) * a.v.stride_t +
-                                                                static_cast<int64_t>(head) * a.v.stride_h);
     const uint32_t kn_b = static_cast<uint32_t>(a.k_nope.stride_t * 2), kr_b = static_cast<uint32_t>(a.k_rope.stride_t * 2),
                    vv_b = static_cast<uint32_t>(a.v.stride_t * 2);
+    const uint8_t* const kn = reinterpret_cast<const uint8_t*>(a.k_nope.data + static_cast<int64_t>(head) * a.k_nope.stride_h) +
+                              static_cast<int64_t>(kv_row) * kn_b;
+    const uint8_t* const kr = reinterpret_cast<const uint8_t*>(a.k_rope.data) + static_cast<int64_t>(kv_row) * kr_b;
+    const uint8_t* const vv = reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(head) * a.v.stride_h) +
+                              static_cast<int64_t>(kv_row) * vv_b;
     const uint32_t lds0 = kc::lds_addr(smem);
+    // A lane's places of the first load of each region; the following loads are
+    // 4 NW (8 NW) rows on, where the swizzle repeats.
+    const int n0 = wave * 64 + lane;
+    const int nrow = n0 >> 4, rrow = n0 >> 3;
+    const uint32_t nc = ((n0 & 15) ^ nope_xor(nrow)) * 16, rc = ((n0 & 7) ^ rope_xor(rrow)) * 16,
+                   vc = ((n0 & 15) ^ value_xor(nrow)) * 16;
+    static_assert((4 * NW) % 16 == 0 || S::nope_loads * 4 * NW <= 16 || NW < 4, "swizzle period");
     // tile from `key`; rows past the range's end re-read its last key
     auto stage = [&](int key, int buf) __attribute__((always_inline)) {
         const int last = key1 - 1 - key;
-        const uint32_t at = lds0 + buf * S::tile;
+        const uint32_t at = lds0 + buf * S::tile + wave * 1024;
+        const uint8_t* const n_base = kn + static_cast<int64_t>(key) * kn_b;
+        const uint8_t* const r_base = kr + static_cast<int64_t>(key) * kr_b;
+        const uint8_t* const v_base = vv + static_cast<int64_t>(key) * vv_b;
+        if (last >= KT - 1 && NW >= 4) {
+            const uint32_t vn = nrow * kn_b + nc, vr = rrow * kr_b + rc, vv_ = nrow * vv_b + vc;
+#pragma unroll
+            for (int i = 0; i < S::nope_loads; ++i)
+                kc::dma16_m0(n_base + static_cast<uint64_t>(i * 4 * NW) * kn_b, vn, at + i * NW * 1024);
+#pragma unroll
+            for (int i = 0; i < S::rope_loads; ++i)
+                kc::dma16_m0(r_base + static_cast<uint64_t>(i * 8 * NW) * kr_b, vr, at + S::rope_at + i * NW * 1024);
+#pragma unroll
+            for (int i = 0; i < S::value_loads; ++i)
+                kc::dma16_m0(v_base + static_cast<uint64_t>(i * 4 * NW) * vv_b, vv_, at + S::value_at + i * NW * 1024);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < S::nope_loads; ++i) {
-            const int n = (i * NW + wave) * 64 + lane, row = n >> 4, c = (n & 15) ^ nope_xor(row);
-            kc::dma16_m0(kn + static_cast<int64_t>(key) * kn_b, static_cast<uint32_t>(min(row, last)) * kn_b + c * 16,
-                         at + (i * NW + wave) * 1024);
+            const int row = nrow + i * 4 * NW, c = (n0 & 15) ^ nope_xor(row);
+            kc::dma16_m0(n_base, static_cast<uint32_t>(min(row, last)) * kn_b + c * 16, at + i * NW * 1024);
         }
 #pragma unroll
         for (int i = 0; i < S::rope_loads; ++i) {
-            const int n = (i * NW + wave) * 64 + lane, row = n >> 3, c = (n & 7) ^ rope_xor(row);
-            kc::dma16_m0(kr + static_cast<int64_t>(key) * kr_b, static_cast<uint32_t>(min(row, last)) * kr_b + c * 16,
-                         at + S::rope_at + (i * NW + wave) * 1024);
+            const int row = rrow + i * 8 * NW, c = (n0 & 7) ^ rope_xor(row);
+            kc::dma16_m0(r_base, static_cast<uint32_t>(min(row, last)) * kr_b + c * 16, at + S::rope_at + i * NW * 1024);
         }
 #pragma unroll
         for (int i = 0; i < S::value_loads; ++i) {
-            const int n = (i * NW + wave) * 64 + lane, row = n >> 4, c = (n & 15) ^ value_xor(row);
-            kc::dma16_m0(vv + static_cast<int64_t>(key) * vv_b, static_cast<uint32_t>(min(row, last)) * vv_b + c * 16,
-                         at + S::value_at + (i * NW + wave) * 1024);
+            const int row = nrow + i * 4 * NW, c = (n0 & 15) ^ value_xor(row);
+            kc::dma16_m0(v_base, static_cast<uint32_t>(min(row, last)) * vv_b + c * 16, at + S::value_at + i * NW * 1024);
         }
     };
     if (key0 < key1) stage(key0, 0);
@@ -172,12 +198,31 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     for (int ks = 0; ks < 12; ++ks)
         q[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
 
-    // ---- LDS read addresses of the lane
-    const int k_nope_at = col * kNopeRow + ((half ^ nope_xor(col)) << 4);                  // ^ (ks << 5)
-    const int k_rope_at = S::rope_at + col * kRopeRow + ((half ^ rope_xor(col)) << 4);     // ^ (ks << 5)
+    // ---- LDS read addresses of the lane, one per swizzled chunk; blocks, steps
+    // and the buffer are immediate offsets
+    const uint8_t* ka[12];
+    const uint8_t* va[4];
     const int tr_row = 4 * half + ((lane & 15) >> 2);
-    const int v_at = S::value_at + tr_row * kValueRow +
-                     (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_xor(tr_row)) << 4) + (lane & 1) * 8;   // ^ (m << 6)
+#pragma unroll
+    for (int ks = 0; ks < 12; ++ks) {
+        int x = ks < 8 ? col * kNopeRow + (((2 * ks + half) ^ nope_xor(col)) << 4)
+                       : S::rope_at + col * kRopeRow + (((2 * (ks - 8) + half) ^ rope_xor(col)) << 4);
+        asm volatile("" : "+v"(x));
+        ka[ks] = smem + x;
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        int x = S::value_at + tr_row * kValueRow +
+                (((4 * m + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_xor(tr_row)) << 4) + (lane & 1) * 8;
+        asm volatile("" : "+v"(x));
+        va[m] = smem + x;
+    }
+    auto value_operand = [&](int off, int ks, int m) __attribute__((always_inline)) {
+        const uint8_t* at = va[m] + off + ks * 16 * kValueRow;
+        const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
+        const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kValueRow));
+        return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 
     f32x16 acc[4];
 #pragma unroll
@@ -187,14 +232,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     float ref = kUnset, sum = 0.0f, rounded = 0.0f;      // sums of the weights, and of the rounded ones
     const float c2 = a.scale_log2;
 
-    int buf = 0;
-    for (int key = key0; key < key1; key += KT, buf ^= 1) {
-        tile_barrier();         // this tile is in LDS; every wave is done with the other buffer
-        if (key + KT < key1) stage(key + KT, buf ^ 1);
-        if (key >= see_max) continue;       // no row of this wave sees any of it
-        const uint8_t* const t = smem + buf * S::tile;
-
-        f32x16 s[KB];
+    // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
+    auto scores = [&](int off, f32x16 (&s)[KB]) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -202,107 +241,144 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
 #pragma unroll
         for (int ks = 0; ks < 12; ++ks)
 #pragma unroll
-            for (int b = 0; b < KB; ++b) {
-                const uint8_t* p = ks < 8 ? t + ((k_nope_at ^ (ks << 5)) + b * 32 * kNopeRow)
-                                          : t + ((k_rope_at ^ ((ks - 8) << 5)) + b * 32 * kRopeRow);
-                s[b] = mfma(*reinterpret_cast<const bf16x8*>(p), q[ks], s[b]);
-            }
-
-        // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
-        const bool masked = key + KT > see_min;
-        if (masked) {
-#pragma unroll
             for (int b = 0; b < KB; ++b)
+                s[b] = mfma(*reinterpret_cast<const bf16x8*>(ka[ks] + off + b * 32 * (ks < 8 ? kNopeRow : kRopeRow)), q[ks], s[b]);
+    };
+    // weights of a tile on the present reference; false if a row's weights went past
+    // what the reference is for
+    auto weigh = [&](const f32x16 (&s)[KB], bf16x8 (&p)[2 * KB], float& tile, float& tile_rounded) __attribute__((always_inline)) {
+        tile = 0.0f;
+        tile_rounded = 0.0f;
+        uint32_t w[8 * KB];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key + 32 * b + (i & 3) + 8 * (i >> 2) + 4 * half >= seen) s[b][i] = -INFINITY;
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -ref));
+                const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], c2, -ref));
+                const uint32_t pair = kc::pack_bf16x2(e0, e1);
+                w[8 * b + (i >> 1)] = pair;
+                tile += e0;
+                tile += e1;
+                tile_rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
+                                                               tile_rounded, false);
+            }
+#pragma unroll
+        for (int k = 0; k < 2 * KB; ++k) {
+            const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
+            p[k] = __builtin_bit_cast(bf16x8, x);
         }
+        return __ballot(!(tile < kMost)) == 0;
+    };
+    // the reference of every row up to its maximum in this tile
+    auto move_reference = [&](const f32x16 (&s)[KB]) __attribute__((always_inline)) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         top = max_halves(top) * c2;
-        if (__ballot(top > ref + kSlack) != 0) {
-            const float next = fminf(fmaxf(ref, top), FLT_MAX);     // (a score of +inf: weight, sum and lse +inf)
-            const float f = exp2f(ref - next);
-            ref = next;
-            sum *= f;
-            rounded *= f;
+        const float next = fminf(fmaxf(ref, top), FLT_MAX);     // (a score of +inf: weight, sum and lse +inf)
+        const float f = exp2f(ref - next);
+        ref = next;
+        sum *= f;
+        rounded *= f;
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[m][i] *= f;
-        }
+            for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+    };
+    auto values = [&](int off, const bf16x8 (&p)[2 * KB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < 2 * KB; ++ks)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[m] = mfma(__builtin_bit_cast(bf16x8, value_operand(off, ks, m)), p[ks], acc[m]);
+    };
+
+    // ---- tiles that every row sees whole
+    int key = key0;
+    const int whole = max(key0, min(see_first, key1));      // (see_first: keys that the block's first row sees)
+    auto step = [&](int off, int buf) __attribute__((always_inline)) {
+        tile_barrier();         // this tile is in LDS; every wave is done with the other buffer
+        if (key + KT < key1) stage(key + KT, buf ^ 1);
+        f32x16 s[KB];
         bf16x8 p[2 * KB];
+        float t, tr;
+        scores(off, s);
+        if (!weigh(s, p, t, tr)) {
+            move_reference(s);
+            weigh(s, p, t, tr);
+        }
+        sum += t;
+        rounded += tr;
+        values(off, p);
+        key += KT;
+    };
+    int buf = 0;
+    while (key + KT <= whole) {
+        step(0, 0);
+        buf = 1;
+        if (key + KT > whole) break;
+        step(S::tile, 1);
+        buf = 0;
+    }
+
+    // ---- the others: the causal limit, the range's end
+    for (; key < key1; key += KT, buf ^= 1) {
+        tile_barrier();
+        if (key + KT < key1) stage(key + KT, buf ^ 1);
+        if (key >= see_max) continue;       // no row of this wave sees any of it
+        const int off = buf * S::tile;
+        f32x16 s[KB];
+        bf16x8 p[2 * KB];
+        float t, tr;
+        scores(off, s);
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -ref));
-                const __bf16 w = static_cast<__bf16>(e);
-                p[2 * b + (i >> 3)][i & 7] = w;
-                sum += e;
-                rounded += static_cast<float>(w);
-            }
+            for (int i = 0; i < 16; ++i)
+                if (key + 32 * b + (i & 3) + 8 * (i >> 2) + 4 * half >= seen) s[b][i] = -INFINITY;
+        if (!weigh(s, p, t, tr)) {
+            move_reference(s);
+            weigh(s, p, t, tr);
+        }
+        sum += t;
+        rounded += tr;
 
         // a key that some row does not see must not reach that row through 0 * inf
         // or 0 * NaN: values that are not finite are left out of the product, and
         // added to the rows that see them (to which they give what they are)
-        bool odd = false;
-        if (masked) {
-            uint32_t found = 0;
+        uint32_t found = 0;
 #pragma unroll
-            for (int i = 0; i < KT * kValueRow / 1024; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4*>(t + S::value_at + i * 1024 + lane * 16);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        for (int i = 0; i < KT * kValueRow / 1024; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(smem + off + S::value_at + i * 1024 + lane * 16);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // an exponent of all ones carries into the sign's place
-                    found |= ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-                }
-            }
-            odd = __ballot(found != 0) != 0;
+            for (int j = 0; j < 4; ++j) found |= ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // an exponent of all ones carries
         }
-        if (!odd) {
+        if (__ballot(found != 0) == 0) {
+            values(off, p);
+            continue;
+        }
 #pragma unroll
-            for (int ks = 0; ks < 2 * KB; ++ks)
+        for (int m = 0; m < 4; ++m) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const uint8_t* at = t + ((v_at ^ (m << 6)) + ks * 16 * kValueRow);
-                    const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
-                    const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kValueRow));
-                    acc[m] = mfma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), p[ks], acc[m]);
-                }
-        } else {
+            for (int ks = 0; ks < 2 * KB; ++ks) {
+                auto v8 = value_operand(off, ks, m);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if ((v8[j] & 0x7F80) == 0x7F80) v8[j] = 0;
+                acc[m] = mfma(__builtin_bit_cast(bf16x8, v8), p[ks], acc[m]);
+            }
 #pragma unroll 1
-            for (int m = 0; m < 4; ++m) {
-                f32x16 o = m == 0 ? acc[0] : m == 1 ? acc[1] : m == 2 ? acc[2] : acc[3];
+            for (int j = 0; j < KT; ++j) {
+                const uint8_t* row = smem + off + S::value_at + j * kValueRow;
 #pragma unroll
-                for (int ks = 0; ks < 2 * KB; ++ks) {
-                    const uint8_t* at = t + ((v_at ^ (m << 6)) + ks * 16 * kValueRow);
-                    const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
-                    const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kValueRow));
-                    auto v8 = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if ((v8[j] & 0x7F80) == 0x7F80) v8[j] = 0;
-                    o = mfma(__builtin_bit_cast(bf16x8, v8), p[ks], o);
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = 32 * m + (i & 3) + 8 * (i >> 2) + 4 * half;
+                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(row + (((ch >> 3) ^ value_xor(j)) << 4) + (ch & 7) * 2);
+                    if ((bits & 0x7F80u) == 0x7F80u && key + j < seen) acc[m][i] += __uint_as_float(bits << 16);
                 }
-#pragma unroll 1
-                for (int j = 0; j < KT; ++j) {
-                    const uint8_t* row = t + S::value_at + j * kValueRow;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int ch = 32 * m + (i & 3) + 8 * (i >> 2) + 4 * half;
-                        const uint32_t bits = *reinterpret_cast<const uint16_t*>(row + (((ch >> 3) ^ value_xor(j)) << 4) + (ch & 7) * 2);
-                        if ((bits & 0x7F80u) == 0x7F80u && key + j < seen) o[i] += __uint_as_float(bits << 16);
-                    }
-                }
-                if (m == 0) acc[0] = o;
-                else if (m == 1) acc[1] = o;
-                else if (m == 2) acc[2] = o;
-                else acc[3] = o;
             }
         }
     }
