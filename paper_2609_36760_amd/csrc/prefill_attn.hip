@@ -26,11 +26,11 @@
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
 // any reference that keeps them far from overflow: a row's is its maximum over
-// its first tile, and it stays until a tile's weights add up to kMost or more
-// (or to no number); then it moves to that tile's maximum, the accumulators
-// follow, and the tile is weighed again.  So the maximum is only looked for in
-// such tiles.  The reference starts at the lowest finite value: hidden scores
-// (-inf) weigh 0 on it, every other overflows and moves it.
+// its first tile, and it stays until a block's weights add up to kMost or more
+// (or to no number); then it moves to that block's maximum, the accumulators
+// follow, and the block is weighed again.  So whole tiles are not searched for
+// maxima.  The reference starts at the lowest finite value, on which hidden
+// scores (-inf) weigh 0.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -48,6 +48,7 @@ using kc::i16x4;
 using kc::lds_i16x4;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kMost = 0x1p30f;
@@ -71,26 +72,24 @@ __device__ __forceinline__ void tile_barrier() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 }
 
-// LDS of one tile: KT rows of 128 nope channels (16 chunks of 16 bytes), KT of
-// 64 RoPE channels (8 chunks), KT of 128 value channels (16 chunks).  Chunk c
-// of row r stands at place c ^ x(r): the score reads (one chunk of 32 rows) and
-// the transposing reads (4 chunks of 8 rows) then touch every bank equally.
-constexpr int kNopeRow = 256, kRopeRow = 128, kValueRow = 256;
-__device__ __forceinline__ int nope_xor(int r) { return r & 15; }
-__device__ __forceinline__ int rope_xor(int r) { return (r >> 1) & 7; }
-__device__ __forceinline__ int value_xor(int r) { return ((r & 3) << 2) | (((r >> 2) & 1) << 1); }
+// LDS of one tile: five planes of 64 channels (128-byte rows) of all KT keys --
+// nope 0-63, nope 64-127, RoPE, values 0-63, values 64-127.  16 bytes c of row r
+// of a plane stand at place c ^ x(r): a read of the same 16 bytes of 32 rows, and
+// a transposing read of 64 bytes of 8 rows, then touch every bank equally.  With
+// planes, a lane's addresses differ by immediate offsets only, but for the
+// swizzled places (4 registers for the scores, 2 for the values).
+constexpr int kRow = 128;
+__device__ __forceinline__ int score_xor(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int value_xor(int r) { return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1; }
 
 template <int NW, int KT>
 struct Shape {
     static constexpr int kb = KT / 32;                      // key blocks of a tile
-    static constexpr int rope_at = KT * kNopeRow;
-    static constexpr int value_at = rope_at + KT * kRopeRow;
-    static constexpr int tile = value_at + KT * kValueRow;
-    // loads of 1 KiB per wave and region
-    static constexpr int nope_loads = KT * kNopeRow / 1024 / NW;
-    static constexpr int rope_loads = KT * kRopeRow / 1024 / NW;
-    static constexpr int value_loads = KT * kValueRow / 1024 / NW;
-    static_assert(rope_loads * 1024 * NW == KT * kRopeRow, "whole loads per wave");
+    static constexpr int plane = KT * kRow;
+    static constexpr int value_at = 3 * plane, tile = 5 * plane;
+    static constexpr int blocks = KT / 8;                   // loads of 1 KiB (8 rows) per plane
+    static constexpr int loads = 5 * blocks / NW;           // per wave
+    static_assert(blocks % NW == 0, "a wave's load belongs to one plane");
 };
 
 template <int NW, int KT>
@@ -144,48 +143,26 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     const uint8_t* const vv = reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(head) * a.v.stride_h) +
                               static_cast<int64_t>(kv_row) * vv_b;
     const uint32_t lds0 = kc::lds_addr(smem);
-    // A lane's places of the first load of each region; the following loads are
-    // 4 NW (8 NW) rows on, where the swizzle repeats.
-    const int n0 = wave * 64 + lane;
-    const int nrow = n0 >> 4, rrow = n0 >> 3;
-    const uint32_t nc = ((n0 & 15) ^ nope_xor(nrow)) * 16, rc = ((n0 & 7) ^ rope_xor(rrow)) * 16,
-                   vc = ((n0 & 15) ^ value_xor(nrow)) * 16;
-    static_assert((4 * NW) % 16 == 0 || S::nope_loads * 4 * NW <= 16 || NW < 4, "swizzle period");
+    // Load i of a wave's part of a tile into LDS byte `to`, from the tile's first
+    // rows n, r, v; row(x) is the row to fetch for the tile's row x.
+    auto load = [&](int lane, int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v, auto row) __attribute__((always_inline)) {
+        const int plane = i * NW / S::blocks, block = i * NW % S::blocks + wave;
+        const int x = block * 8 + (lane >> 3);
+        const uint32_t c = static_cast<uint32_t>((lane & 7) ^ (plane < 3 ? score_xor(x) : value_xor(x))) * 16;
+        const uint32_t at = lds0 + to + plane * S::plane + block * 1024;
+        if (plane < 2) kc::dma16_m0(n + plane * kRow, row(x) * kn_b + c, at);
+        else if (plane == 2) kc::dma16_m0(r, row(x) * kr_b + c, at);
+        else kc::dma16_m0(v + (plane - 3) * kRow, row(x) * vv_b + c, at);
+    };
     // tile from `key`; rows past the range's end re-read its last key
-    auto stage = [&](int key, int buf) __attribute__((always_inline)) {
+    auto stage = [&](int key, int to) __attribute__((always_inline)) {
         const int last = key1 - 1 - key;
-        const uint32_t at = lds0 + buf * S::tile + wave * 1024;
-        const uint8_t* const n_base = kn + static_cast<int64_t>(key) * kn_b;
-        const uint8_t* const r_base = kr + static_cast<int64_t>(key) * kr_b;
-        const uint8_t* const v_base = vv + static_cast<int64_t>(key) * vv_b;
-        if (last >= KT - 1 && NW >= 4) {
-            const uint32_t vn = nrow * kn_b + nc, vr = rrow * kr_b + rc, vv_ = nrow * vv_b + vc;
+        int l = lane;
+        asm volatile("" : "+v"(l));         // (what follows from it is not worth registers across the loops)
 #pragma unroll
-            for (int i = 0; i < S::nope_loads; ++i)
-                kc::dma16_m0(n_base + static_cast<uint64_t>(i * 4 * NW) * kn_b, vn, at + i * NW * 1024);
-#pragma unroll
-            for (int i = 0; i < S::rope_loads; ++i)
-                kc::dma16_m0(r_base + static_cast<uint64_t>(i * 8 * NW) * kr_b, vr, at + S::rope_at + i * NW * 1024);
-#pragma unroll
-            for (int i = 0; i < S::value_loads; ++i)
-                kc::dma16_m0(v_base + static_cast<uint64_t>(i * 4 * NW) * vv_b, vv_, at + S::value_at + i * NW * 1024);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < S::nope_loads; ++i) {
-            const int row = nrow + i * 4 * NW, c = (n0 & 15) ^ nope_xor(row);
-            kc::dma16_m0(n_base, static_cast<uint32_t>(min(row, last)) * kn_b + c * 16, at + i * NW * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < S::rope_loads; ++i) {
-            const int row = rrow + i * 8 * NW, c = (n0 & 7) ^ rope_xor(row);
-            kc::dma16_m0(r_base, static_cast<uint32_t>(min(row, last)) * kr_b + c * 16, at + S::rope_at + i * NW * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < S::value_loads; ++i) {
-            const int row = nrow + i * 4 * NW, c = (n0 & 15) ^ value_xor(row);
-            kc::dma16_m0(v_base, static_cast<uint32_t>(min(row, last)) * vv_b + c * 16, at + S::value_at + i * NW * 1024);
-        }
+        for (int i = 0; i < S::loads; ++i)
+            load(l, i, to, kn + static_cast<int64_t>(key) * kn_b, kr + static_cast<int64_t>(key) * kr_b,
+                 vv + static_cast<int64_t>(key) * vv_b, [&](int x) { return static_cast<uint32_t>(min(x, last)); });
     };
     if (key0 < key1) stage(key0, 0);
 
@@ -198,29 +175,32 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     for (int ks = 0; ks < 12; ++ks)
         q[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
 
-    // ---- LDS read addresses of the lane, one per swizzled chunk; blocks, steps
-    // and the buffer are immediate offsets
-    const uint8_t* ka[12];
-    const uint8_t* va[4];
+    // (waited for here: the wait that the compiler would put into the loop, for
+    // its first pass, would hold every pass up until the next tile is staged)
+#pragma unroll
+    for (int ks = 0; ks < 12; ++ks) asm volatile("" : "+v"(q[ks]));
+
+    // ---- LDS read addresses of the lane; planes, blocks and steps are immediate
+    // offsets
+    int ka[4], va[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ka[j] = col * kRow + (((2 * j + half) ^ score_xor(col)) << 4);
+    // the transposing read: 16 lanes fetch 4 rows x 16 channels, 8 bytes each
     const int tr_row = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) {
-        int x = ks < 8 ? col * kNopeRow + (((2 * ks + half) ^ nope_xor(col)) << 4)
-                       : S::rope_at + col * kRopeRow + (((2 * (ks - 8) + half) ^ rope_xor(col)) << 4);
+    for (int j = 0; j < 2; ++j)
+        va[j] = S::value_at + tr_row * kRow + (((4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_xor(tr_row)) << 4) +
+                (lane & 1) * 8;
+    // (the base of an LDS access is a register that the tile's place is added to once)
+    auto at_tile = [&](int x, int off) __attribute__((always_inline)) {
+        x += off;
         asm volatile("" : "+v"(x));
-        ka[ks] = smem + x;
-    }
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        int x = S::value_at + tr_row * kValueRow +
-                (((4 * m + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_xor(tr_row)) << 4) + (lane & 1) * 8;
-        asm volatile("" : "+v"(x));
-        va[m] = smem + x;
-    }
-    auto value_operand = [&](int off, int ks, int m) __attribute__((always_inline)) {
-        const uint8_t* at = va[m] + off + ks * 16 * kValueRow;
+        return x;
+    };
+    auto value_operand = [&](const int (&base)[2], int ks, int m) __attribute__((always_inline)) {
+        const uint8_t* at = smem + base[m & 1] + (m >> 1) * S::plane + ks * 16 * kRow;
         const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
-        const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kValueRow));
+        const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kRow));
         return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
@@ -233,153 +213,205 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     const float c2 = a.scale_log2;
 
     // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
-    auto scores = [&](int off, f32x16 (&s)[KB]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < 12; ++ks)
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-                s[b] = mfma(*reinterpret_cast<const bf16x8*>(ka[ks] + off + b * 32 * (ks < 8 ? kNopeRow : kRopeRow)), q[ks], s[b]);
+    f32x16 s[KB];
+    uint32_t w[8 * KB];         // weights, bf16 pairs
+    float tile, tile_rounded;   // sums of a block's weights
+    auto key_operand = [&](const int (&base)[4], int st) __attribute__((always_inline)) {
+        const int b = st / 12, ks = st % 12;
+        return *reinterpret_cast<const bf16x8*>(smem + base[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow);
     };
-    // weights of a tile on the present reference; false if a row's weights went past
-    // what the reference is for
-    auto weigh = [&](const f32x16 (&s)[KB], bf16x8 (&p)[2 * KB], float& tile, float& tile_rounded) __attribute__((always_inline)) {
-        tile = 0.0f;
-        tile_rounded = 0.0f;
-        uint32_t w[8 * KB];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -ref));
-                const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], c2, -ref));
-                const uint32_t pair = kc::pack_bf16x2(e0, e1);
-                w[8 * b + (i >> 1)] = pair;
-                tile += e0;
-                tile += e1;
-                tile_rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
-                                                               tile_rounded, false);
-            }
-#pragma unroll
-        for (int k = 0; k < 2 * KB; ++k) {
-            const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
-            p[k] = __builtin_bit_cast(bf16x8, x);
-        }
-        return __ballot(!(tile < kMost)) == 0;
+    auto score = [&](int st, bf16x8 k) __attribute__((always_inline)) {
+        const int b = st / 12, ks = st % 12;
+        const f32x16 zero = {};
+        s[b] = mfma(k, q[ks], ks == 0 ? zero : s[b]);
     };
-    // the reference of every row up to its maximum in this tile
-    auto move_reference = [&](const f32x16 (&s)[KB]) __attribute__((always_inline)) {
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max_halves(top) * c2;
-        const float next = fminf(fmaxf(ref, top), FLT_MAX);     // (a score of +inf: weight, sum and lse +inf)
-        const float f = exp2f(ref - next);
-        ref = next;
-        sum *= f;
-        rounded *= f;
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+    // weights of registers 2j, 2j + 1 of block b on the present reference
+    auto weigh = [&](int b, int j) __attribute__((always_inline)) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * j], c2, -ref));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * j + 1], c2, -ref));
+        const uint32_t pair = kc::pack_bf16x2(e0, e1);
+        w[8 * b + j] = pair;
+        tile = j == 0 ? e0 : tile + e0;
+        tile += e1;
+        tile_rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
+                                                       j == 0 ? 0.0f : tile_rounded, false);
+        // (computed here: the compiler would sink it behind the next branch)
+        asm volatile("" : "+v"(w[8 * b + j]), "+v"(tile), "+v"(tile_rounded));
     };
-    auto values = [&](int off, const bf16x8 (&p)[2 * KB]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int ks = 0; ks < 2 * KB; ++ks)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) acc[m] = mfma(__builtin_bit_cast(bf16x8, value_operand(off, ks, m)), p[ks], acc[m]);
+    auto weights = [&](int ks) __attribute__((always_inline)) {
+        const u32x4 x = {w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3]};
+        return __builtin_bit_cast(bf16x8, x);
     };
+    auto too_large = [&]() __attribute__((always_inline)) { return __ballot(!(tile < kMost)) != 0; };
 
-    // ---- tiles that every row sees whole
-    int key = key0;
-    const int whole = max(key0, min(see_first, key1));      // (see_first: keys that the block's first row sees)
-    auto step = [&](int off, int buf) __attribute__((always_inline)) {
-        tile_barrier();         // this tile is in LDS; every wave is done with the other buffer
-        if (key + KT < key1) stage(key + KT, buf ^ 1);
-        f32x16 s[KB];
-        bf16x8 p[2 * KB];
-        float t, tr;
-        scores(off, s);
-        if (!weigh(s, p, t, tr)) {
-            move_reference(s);
-            weigh(s, p, t, tr);
-        }
-        sum += t;
-        rounded += tr;
-        values(off, p);
-        key += KT;
-    };
-    int buf = 0;
-    while (key + KT <= whole) {
-        step(0, 0);
-        buf = 1;
-        if (key + KT > whole) break;
-        step(S::tile, 1);
-        buf = 0;
-    }
-
-    // ---- the others: the causal limit, the range's end
-    for (; key < key1; key += KT, buf ^= 1) {
-        tile_barrier();
-        if (key + KT < key1) stage(key + KT, buf ^ 1);
-        if (key >= see_max) continue;       // no row of this wave sees any of it
-        const int off = buf * S::tile;
-        f32x16 s[KB];
-        bf16x8 p[2 * KB];
-        float t, tr;
-        scores(off, s);
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (key + 32 * b + (i & 3) + 8 * (i >> 2) + 4 * half >= seen) s[b][i] = -INFINITY;
-        if (!weigh(s, p, t, tr)) {
-            move_reference(s);
-            weigh(s, p, t, tr);
-        }
-        sum += t;
-        rounded += tr;
-
+    // Any tile (its operands at kt, vt), from block `from` on: the causal limit, the
+    // range's end, references that move.
+    auto any_tile = [&](int key, int off, int from) __attribute__((always_inline)) {
+        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
+        const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
+        const int seen_here = seen - key - 4 * half;
         // a key that some row does not see must not reach that row through 0 * inf
         // or 0 * NaN: values that are not finite are left out of the product, and
         // added to the rows that see them (to which they give what they are)
         uint32_t found = 0;
+        if (key + KT > see_first) {
 #pragma unroll
-        for (int i = 0; i < KT * kValueRow / 1024; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(smem + off + S::value_at + i * 1024 + lane * 16);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            for (int i = 0; i < 2 * S::plane / 1024; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4*>(smem + off + S::value_at + i * 1024 + lane * 16);
+                const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) found |= ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // an exponent of all ones carries
-        }
-        if (__ballot(found != 0) == 0) {
-            values(off, p);
-            continue;
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-#pragma unroll
-            for (int ks = 0; ks < 2 * KB; ++ks) {
-                auto v8 = value_operand(off, ks, m);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if ((v8[j] & 0x7F80) == 0x7F80) v8[j] = 0;
-                acc[m] = mfma(__builtin_bit_cast(bf16x8, v8), p[ks], acc[m]);
+                for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // an exponent of all ones carries
             }
+        }
+        const bool odd = __ballot(found != 0) != 0;
+        auto block = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+            for (int ks = 0; ks < 12; ++ks) score(12 * b + ks, key_operand(kt, 12 * b + ks));
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * b + (i & 3) + 8 * (i >> 2) >= seen_here) s[b][i] = -INFINITY;
+            float top = s[b][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
+            top = max_halves(top) * c2;
+            if (__ballot(top > ref) != 0) {
+                const float next = fminf(fmaxf(ref, top), FLT_MAX);     // (a score of +inf: weight, sum and lse +inf)
+                const float f = __builtin_amdgcn_exp2f(ref - next);
+                ref = next;
+                sum *= f;
+                rounded *= f;
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) weigh(b, j);
+            sum += tile;
+            rounded += tile_rounded;
+#pragma unroll
+            for (int st = 8 * b; st < 8 * b + 8; ++st) {
+                auto v8 = value_operand(vt, st >> 2, st & 3);
+                if (odd) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if ((v8[j] & 0x7F80) == 0x7F80) v8[j] = 0;
+                }
+                acc[st & 3] = mfma(__builtin_bit_cast(bf16x8, v8), weights(st >> 2), acc[st & 3]);
+            }
+        };
+        if (from == 0) block(0);
+        if constexpr (KB == 2) block(1);
+        if (!odd) return;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
 #pragma unroll 1
-            for (int j = 0; j < KT; ++j) {
-                const uint8_t* row = smem + off + S::value_at + j * kValueRow;
+            for (int j = 32 * from; j < KT; ++j) {
+                const uint8_t* row = smem + off + S::value_at + (m >> 1) * S::plane + j * kRow;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int ch = 32 * m + (i & 3) + 8 * (i >> 2) + 4 * half;
-                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(row + (((ch >> 3) ^ value_xor(j)) << 4) + (ch & 7) * 2);
+                    const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
+                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(row + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
                     if ((bits & 0x7F80u) == 0x7F80u && key + j < seen) acc[m][i] += __uint_as_float(bits << 16);
                 }
             }
+    };
+
+    // The loads of a whole tile: a wave's are a swizzle period (16 rows) apart, or
+    // half of one, so a lane has two offsets per kind of row, and the rest is scalar.
+    const int x0 = wave * 8 + (lane >> 3);
+    const uint32_t c0 = ((lane & 7) ^ score_xor(x0)) * 16;
+    const uint32_t at_n[2] = {x0 * kn_b + c0, x0 * kn_b + (c0 ^ 64)}, at_r[2] = {x0 * kr_b + c0, x0 * kr_b + (c0 ^ 64)};
+    const uint32_t at_v = x0 * vv_b + ((lane & 7) ^ value_xor(x0)) * 16;
+    auto load_whole = [&](int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v) __attribute__((always_inline)) {
+        const int plane = i * NW / S::blocks, first = i * NW % S::blocks;
+        const uint32_t at = lds0 + to + plane * S::plane + (first + wave) * 1024;
+        if (plane < 2) kc::dma16_m0(n + plane * kRow + static_cast<uint64_t>(first * 8) * kn_b, at_n[first & 1], at);
+        else if (plane == 2) kc::dma16_m0(r + static_cast<uint64_t>(first * 8) * kr_b, at_r[first & 1], at);
+        else kc::dma16_m0(v + (plane - 3) * kRow + static_cast<uint64_t>(first * 8) * vv_b, at_v, at);
+    };
+
+    // One tile by any_tile, then as many as there are that every row sees whole, with
+    // another whole tile behind them, until one's weights are too large for a
+    // reference: that one goes to any_tile again, from its block on.
+    //
+    // A slot is one matrix instruction and what is issued in its shadow: the operand
+    // read of a later slot, a load of the next tile, a piece of the softmax.  The
+    // scheduling barriers keep that order.  (Moving the reference here would make the
+    // compiler copy the accumulators in every tile.)
+    const int whole = min(see_first, key1 - KT);        // (see_first: keys that the block's first row sees)
+    int key = key0, off = 0, from = 0;
+    bool entered = false;
+    while (key < key1) {
+        if (!entered) {
+            tile_barrier();         // this tile is in LDS; every wave is done with the other buffer
+            if (key + KT < key1) stage(key + KT, S::tile - off);
+        }
+        if (key < see_max) any_tile(key, off, from);    // (else no row of this wave sees any of it)
+        entered = false;
+        from = 0;
+        key += KT;
+        off = S::tile - off;
+
+        constexpr int kScores = 12 * KB, kValues = 8 * KB, kAhead = 4;
+        static_assert(S::loads <= kScores || NW == 1, "loads of the next tile in the score slots");
+        while (key + KT <= whole) {
+            tile_barrier();
+            const uint32_t to = S::tile - off;
+            const uint8_t* const next_n = kn + static_cast<int64_t>(key + KT) * kn_b;
+            const uint8_t* const next_r = kr + static_cast<int64_t>(key + KT) * kr_b;
+            const uint8_t* const next_v = vv + static_cast<int64_t>(key + KT) * vv_b;
+            const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
+            const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
+            bf16x8 k[kAhead];
+            i16x8 v[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) k[j] = key_operand(kt, j);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int st = 0; st < kScores; ++st) {
+                score(st, k[st % kAhead]);
+                if (st + kAhead < kScores) k[st % kAhead] = key_operand(kt, st + kAhead);
+                else v[st + kAhead - kScores] = value_operand(vt, 0, st + kAhead - kScores);
+#pragma unroll
+                for (int i = st; i < S::loads; i += kScores) load_whole(i, to, next_n, next_r, next_v);
+                if (KB == 2 && st >= 14 && st < 22) weigh(0, st - 14);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (KB == 1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) weigh(0, j);
+            }
+            entered = too_large();
+            if (entered) break;
+            sum += tile;
+            rounded += tile_rounded;
+            __builtin_amdgcn_sched_barrier(0);
+            auto values = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+                for (int st = 8 * b; st < 8 * b + 8; ++st) {
+                    const int m = st & 3;
+                    acc[m] = mfma(__builtin_bit_cast(bf16x8, v[st % kAhead]), weights(st >> 2), acc[m]);
+                    if (st + kAhead < kValues) v[st % kAhead] = value_operand(vt, (st + kAhead) >> 2, m);
+                    if (b + 1 < KB && st > 0) weigh(b + 1, st - 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            values(0);
+            if constexpr (KB == 2) {
+                weigh(1, 7);
+                if (too_large()) {
+                    entered = true;
+                    from = 1;
+                    break;
+                }
+                sum += tile;
+                rounded += tile_rounded;
+                __builtin_amdgcn_sched_barrier(0);
+                values(1);
+            }
+            key += KT;
+            off = S::tile - off;
         }
     }
 
