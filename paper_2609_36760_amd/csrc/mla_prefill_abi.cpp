@@ -157,12 +157,12 @@ int32_t splits_of(int32_t tiles, int64_t most) {
 struct Shape {
     int32_t rows, slots, least_tiles;
 };
-constexpr Shape kShapes[] = {{32, 1024, 4}, {128, 512, 8}};
+constexpr Shape kShapes[] = {{32, 512, 4}, {128, 256, 8}, {256, 256, 8}};
 
 Shape choose_rows(const Lengths& n) {
     int32_t most = 0;
     for (int32_t b = 0; b < n.B; ++b) most = std::max(most, n.q[b]);
-    return most <= 32 ? kShapes[0] : kShapes[1];
+    return most <= 32 ? kShapes[0] : most <= 128 ? kShapes[1] : kShapes[2];
 }
 
 int check_lengths(const Lengths& n, int64_t* total_q, int64_t* total_kv) {

@@ -2,21 +2,30 @@
 // q_rope . k_rope)) v over 192 score channels (64 of them one key row for all
 // heads) and 128 value channels, for blocks of query rows.
 //
-// One workgroup takes a plan's work item for one head: 32 query rows per wave,
-// all waves over the same key tiles.  Per tile of KT keys (KT / 32 key blocks):
-//   1. the tile's rows go from memory straight into LDS, one tile ahead, 16
+// One workgroup takes a plan's work item for one head: G groups of 32 query rows
+// per wave, all waves over the same key tiles.  Per tile of KT keys (KT / 32 key
+// blocks):
+//   1. the tile's rows go from memory straight into LDS, two tiles ahead, 16
 //      bytes a lane; LDS places are linear in the lane, so the bank swizzle is
 //      applied to which 16 bytes of a row a lane fetches;
-//   2. S^T[key][row] = K . Q^T, v_mfma_f32_32x32x16_bf16 (M = 32 keys, N = the
-//      wave's 32 rows, K = 192 channels in 12 steps), Q^T in registers
-//      throughout: a lane ends up with one row's scores for half of the keys,
-//      its partner lane ^ 32 with the other half;
+//   2. S^T[key][row] = K . Q^T, v_mfma_f32_32x32x16_bf16 (M = 32 keys, N = 32
+//      rows, K = 192 channels in 12 steps), Q^T in registers throughout: a lane
+//      ends up with one row's scores for half of the keys, its partner lane ^ 32
+//      with the other half;
 //   3. one pass over the scores: weights 2^(s - reference) in fp32 on the row's
 //      running reference, rounded to bf16, their sums;
 //   4. O^T[channel][row] += V^T . P^T (M = 128 channels in 4 blocks, K = KT
 //      keys): P^T comes straight from the score registers, because the
 //      transposing LDS reads fetch V's keys in the order in which the score
 //      product left them.
+//
+// What bounds it is the matrix unit, and the power that everything around it
+// draws (the clock falls from 2.4 to 1.65 GHz under the two-waves-per-SIMD form
+// of this kernel).  So a wave has two row groups where there are rows enough:
+// every operand read from LDS feeds two products, every tile staged 256 rows.
+// Such a wave has a SIMD to itself (acc 128, Q 96, scores 64, weights 32
+// registers), and overlaps by its own instruction order: the softmax of one key
+// block runs between the products of the next.
 //
 // Roundings: the weights are bf16 operands of the second product (at most 2^-8
 // of a weight, as the bf16 output's own rounding).  The output is normalized by
@@ -28,12 +37,13 @@
 // any reference that keeps them far from overflow: a row's is its maximum over
 // its first tile, and it stays until a block's weights add up to kMost or more
 // (or to no number); then it moves to that block's maximum, the accumulators
-// follow, and the block is weighed again.  So whole tiles are not searched for
-// maxima.  The reference starts at the lowest finite value, on which hidden
+// follow, and the block is weighed again.  So tiles are not searched for maxima
+// as a rule.  The reference starts at the lowest finite value, on which hidden
 // scores (-inf) weigh 0.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
+#include <type_traits>
 
 #include "internal.h"
 #include "kernel_common.h"
@@ -57,6 +67,18 @@ constexpr float kUnset = -FLT_MAX;
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+// Score products accumulate in vector registers: kept with the output in the
+// accumulation registers, the compiler would copy every score out.  As inline
+// assembly they get no wait states: the first product of a chain writes without
+// reading, the following ones accumulate back to back (no wait between products
+// of one shape), and scores_ready supplies the wait before vector instructions
+// read the result (12 wait states after a 32 x 32 x 16 product).  The queries
+// stay in accumulation registers, beside the output.
+__device__ __forceinline__ void score_mfma(f32x16& c, bf16x8 a, bf16x8 b, bool first) {
+    if (first) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void scores_ready(f32x16& c) { asm volatile("s_nop 7\n\ts_nop 7" : "+v"(c)); }
 
 // Maximum / sum of a value and its copy in lane ^ 32.
 __device__ __forceinline__ float max_halves(float v) {
@@ -68,8 +90,27 @@ __device__ __forceinline__ float sum_halves(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ void tile_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+// Output accumulators changed outside the products: in place, in their
+// accumulation registers (as ordinary arithmetic, the compiler would move all of
+// them to vector registers and back around every use).  It places no wait states
+// around these either: acc_wait stands between products and what follows.
+__device__ __forceinline__ void acc_wait(f32x16 (&c)[4]) {
+    asm volatile("s_nop 15\n\ts_nop 7" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]));
+}
+__device__ __forceinline__ void acc_scale(f32x16 (&c)[4], float f) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float t;
+            asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                         : "+a"(c[m][i]), "=&v"(t) : "v"(f));
+        }
+}
+__device__ __forceinline__ void acc_add(f32x16& c, int i, float x) {
+    float t;
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_add_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                 : "+a"(c[i]), "=&v"(t) : "v"(x));
 }
 
 // LDS of one tile: five planes of 64 channels (128-byte rows) of all KT keys --
@@ -82,21 +123,27 @@ constexpr int kRow = 128;
 __device__ __forceinline__ int score_xor(int r) { return (r >> 1) & 7; }
 __device__ __forceinline__ int value_xor(int r) { return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1; }
 
-template <int NW, int KT>
+// NW waves of G row groups over tiles of KT keys.
+template <int NW, int G, int KT>
 struct Shape {
+    static constexpr int rows = NW * G * kRowsPerWave;
     static constexpr int kb = KT / 32;                      // key blocks of a tile
     static constexpr int plane = KT * kRow;
     static constexpr int value_at = 3 * plane, tile = 5 * plane;
     static constexpr int blocks = KT / 8;                   // loads of 1 KiB (8 rows) per plane
     static constexpr int loads = 5 * blocks / NW;           // per wave
     static_assert(blocks % NW == 0, "a wave's load belongs to one plane");
+    static constexpr int buffers = 3;
+    static constexpr int lds = buffers * tile + buffers * NW * 4;
+    static_assert(lds <= 160 * 1024 && NW * G * kRowsPerWave * 256 <= (buffers - 1) * tile, "LDS; results beside the last tile");
 };
 
-template <int NW, int KT>
-__global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
-    using S = Shape<NW, KT>;
+template <int NW, int G, int KT>
+__global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
+    using S = Shape<NW, G, KT>;
     constexpr int KB = S::kb;
-    __shared__ __align__(1024) uint8_t smem[2 * S::tile];
+    __shared__ __align__(1024) uint8_t smem[S::lds];
+    volatile uint32_t* const flags = reinterpret_cast<volatile uint32_t*>(smem + S::buffers * S::tile);
 
     const int lane = static_cast<int>(threadIdx.x) & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -119,20 +166,19 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     const PrefillItem* ip = a.items + item_id;
     // indices from the plan, kept inside the tensors whatever it holds
     const int q_row = min(max(ip->q_row, 0), a.total_q - 1);
-    const int q_rows = min(min(max(ip->q_rows, 1), NW * kRowsPerWave), a.total_q - q_row);
+    const int q_rows = min(min(max(ip->q_rows, 1), S::rows), a.total_q - q_row);
     const int kv_row = min(max(ip->kv_row, 0), a.total_kv);
     const int key1 = min(max(ip->key1, 0), a.total_kv - kv_row);
     const int key0 = min(max(ip->key0, 0), key1);
     const int seen0 = ip->seen0;
     const int part = min(ip->part, a.num_parts - 1);
 
-    const int r = wave * kRowsPerWave + col;        // the lane's row of the block
-    const int seen = static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + r));
-    const int see_first = static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0)));   // of row 0
-    // the most keys that a row of this wave sees (rows that exist)
-    const int r_first = wave * kRowsPerWave, r_last = min(r_first + kRowsPerWave, q_rows) - 1;
-    const int see_max = r_last < r_first ? key0
-                                         : static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + r_last));
+    // keys that row x of the block sees
+    auto sees = [&](int x) { return static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + x)); };
+    const int r0 = wave * G * kRowsPerWave;         // the wave's first row of the block
+    const int see_block = sees(0), see_first = sees(r0);
+    const int r_last = min(r0 + G * kRowsPerWave, q_rows) - 1;
+    const int see_last = r_last < r0 ? key0 : sees(r_last);     // the most keys that a row of this wave sees
 
     // ---- staging ----------------------------------------------------------
     const uint32_t kn_b = static_cast<uint32_t>(a.k_nope.stride_t * 2), kr_b = static_cast<uint32_t>(a.k_rope.stride_t * 2),
@@ -143,42 +189,98 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
     const uint8_t* const vv = reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(head) * a.v.stride_h) +
                               static_cast<int64_t>(kv_row) * vv_b;
     const uint32_t lds0 = kc::lds_addr(smem);
-    // Load i of a wave's part of a tile into LDS byte `to`, from the tile's first
-    // rows n, r, v; row(x) is the row to fetch for the tile's row x.
-    auto load = [&](int lane, int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v, auto row) __attribute__((always_inline)) {
-        const int plane = i * NW / S::blocks, block = i * NW % S::blocks + wave;
-        const int x = block * 8 + (lane >> 3);
-        const uint32_t c = static_cast<uint32_t>((lane & 7) ^ (plane < 3 ? score_xor(x) : value_xor(x))) * 16;
-        const uint32_t at = lds0 + to + plane * S::plane + block * 1024;
-        if (plane < 2) kc::dma16_m0(n + plane * kRow, row(x) * kn_b + c, at);
-        else if (plane == 2) kc::dma16_m0(r, row(x) * kr_b + c, at);
-        else kc::dma16_m0(v + (plane - 3) * kRow, row(x) * vv_b + c, at);
-    };
-    // tile from `key`; rows past the range's end re-read its last key
+    // A wave's loads of a tile: i * NW + wave counts the tile's 8-row blocks, plane by
+    // plane.  Rows past the range's end re-read its last key.
     auto stage = [&](int key, int to) __attribute__((always_inline)) {
         const int last = key1 - 1 - key;
         int l = lane;
         asm volatile("" : "+v"(l));         // (what follows from it is not worth registers across the loops)
+        const uint8_t* const n = kn + static_cast<int64_t>(key) * kn_b;
+        const uint8_t* const r = kr + static_cast<int64_t>(key) * kr_b;
+        const uint8_t* const v = vv + static_cast<int64_t>(key) * vv_b;
 #pragma unroll
-        for (int i = 0; i < S::loads; ++i)
-            load(l, i, to, kn + static_cast<int64_t>(key) * kn_b, kr + static_cast<int64_t>(key) * kr_b,
-                 vv + static_cast<int64_t>(key) * vv_b, [&](int x) { return static_cast<uint32_t>(min(x, last)); });
+        for (int i = 0; i < S::loads; ++i) {
+            const int plane = i * NW / S::blocks, block = i * NW % S::blocks + wave;
+            const int x = block * 8 + (l >> 3);
+            const uint32_t row = static_cast<uint32_t>(min(x, last));
+            const uint32_t c = static_cast<uint32_t>((l & 7) ^ (plane < 3 ? score_xor(x) : value_xor(x))) * 16;
+            const uint32_t at = lds0 + to + plane * S::plane + block * 1024;
+            if (plane < 2) kc::dma16_m0(n + plane * kRow, row * kn_b + c, at);
+            else if (plane == 2) kc::dma16_m0(r, row * kr_b + c, at);
+            else kc::dma16_m0(v + (plane - 3) * kRow, row * vv_b + c, at);
+        }
+    };
+    // Load i of a tile that is there whole: a wave's loads are a swizzle period (16
+    // rows) apart, or half of one, so a lane has two offsets per kind of row, and the
+    // rest is scalar.
+    const int x0 = wave * 8 + (lane >> 3);
+    const uint32_t c0 = ((lane & 7) ^ score_xor(x0)) * 16;
+    const uint32_t at_n[2] = {x0 * kn_b + c0, x0 * kn_b + (c0 ^ 64)}, at_r[2] = {x0 * kr_b + c0, x0 * kr_b + (c0 ^ 64)};
+    const uint32_t at_v = x0 * vv_b + ((lane & 7) ^ value_xor(x0)) * 16;
+    auto load_whole = [&](int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v) __attribute__((always_inline)) {
+        const int plane = i * NW / S::blocks, first = i * NW % S::blocks;
+        const uint32_t at = lds0 + to + plane * S::plane + (first + wave) * 1024;
+        if (plane < 2) kc::dma16_m0(n + plane * kRow + static_cast<uint64_t>(first * 8) * kn_b, at_n[first & 1], at);
+        else if (plane == 2) kc::dma16_m0(r + static_cast<uint64_t>(first * 8) * kr_b, at_r[first & 1], at);
+        else kc::dma16_m0(v + (plane - 3) * kRow + static_cast<uint64_t>(first * 8) * vv_b, at_v, at);
+    };
+    // A value that some row does not see must not reach that row through 0 * inf or
+    // 0 * NaN.  A wave looks through the values that it staged itself, once they are
+    // there, of the tiles that some row sees in part; `flags` says whether any wave
+    // found one that is not finite (the buffer's NW words).
+    auto look = [&](int key, int to) __attribute__((always_inline)) {
+        if (key + KT <= see_block) return;
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < S::loads; ++i) {
+            const int plane = i * NW / S::blocks, block = i * NW % S::blocks + wave;
+            if (plane < 3) continue;
+            const uint4 x = *reinterpret_cast<const uint4*>(smem + to + plane * S::plane + block * 1024 + lane * 16);
+            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // an exponent of all ones carries
+        }
+        const uint32_t any = __ballot(found != 0) != 0;
+        if (lane == 0) flags[to / S::tile * NW + wave] = any;
+    };
+    auto odd_values = [&](int off) __attribute__((always_inline)) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) any |= flags[off / S::tile * NW + i];
+        return __builtin_amdgcn_readfirstlane(any) != 0;
+    };
+    // Buffers are used in turn: tile j + 2 goes where tile j - 1 was.
+    auto after = [&](int off) __attribute__((always_inline)) { return off == (S::buffers - 1) * S::tile ? 0 : off + S::tile; };
+    // Once per tile, anywhere in a wave's work on it: the next tile is there, and no
+    // wave reads the one before any more.
+    auto meet = [&](int key, int off) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        if (key + KT < key1) look(key + KT, after(off));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    };
+    auto stage_ahead = [&](int key, int off) __attribute__((always_inline)) {
+        if (key + 2 * KT < key1) stage(key + 2 * KT, after(after(off)));
     };
     if (key0 < key1) stage(key0, 0);
 
-    // ---- queries: operand B of step ks holds channels 16 ks + 8 half .. + 7 of row `col`
-    const int64_t qr = q_row + min(r, q_rows - 1);
-    const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(head) * a.q_nope.stride_h + 8 * half;
-    const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(head) * a.q_rope.stride_h + 8 * half;
-    bf16x8 q[12];
+    // ---- queries: operand B of step ks holds channels 16 ks + 8 half .. + 7 of the
+    // lane's row of the group
+    bf16x8 q[G][12];
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks)
-        q[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
-
+    for (int g = 0; g < G; ++g) {
+        const int64_t qr = q_row + min(r0 + 32 * g + col, q_rows - 1);
+        const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(head) * a.q_nope.stride_h + 8 * half;
+        const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(head) * a.q_rope.stride_h + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < 12; ++ks)
+            q[g][ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
+    }
     // (waited for here: the wait that the compiler would put into the loop, for
     // its first pass, would hold every pass up until the next tile is staged)
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) asm volatile("" : "+v"(q[ks]));
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int ks = 0; ks < 12; ++ks) asm volatile("" : "+a"(q[g][ks]));
 
     // ---- LDS read addresses of the lane; planes, blocks and steps are immediate
     // offsets
@@ -197,257 +299,358 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a) {
         asm volatile("" : "+v"(x));
         return x;
     };
-    auto value_operand = [&](const int (&base)[2], int ks, int m) __attribute__((always_inline)) {
+    // operand A: keys of block st / 12, channels of step st % 12
+    auto key_operand = [&](const int (&base)[4], int st) __attribute__((always_inline)) {
+        const int b = st / 12, ks = st % 12;
+        return *reinterpret_cast<const bf16x8*>(smem + base[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow);
+    };
+    // operand A: channels of block m = st % 4, the 16 keys of step st / 4
+    auto value_operand = [&](const int (&base)[2], int st) __attribute__((always_inline)) {
+        const int ks = st >> 2, m = st & 3;
         const uint8_t* at = smem + base[m & 1] + (m >> 1) * S::plane + ks * 16 * kRow;
         const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
         const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kRow));
         return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
-    f32x16 acc[4];
+    f32x16 acc[G][4];
+    float ref[G], sum[G], rounded[G];       // reference; sums of the weights, and of the rounded ones
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int g = 0; g < G; ++g) {
+        ref[g] = kUnset;
+        sum[g] = rounded[g] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[m][i] = 0.0f;
-    float ref = kUnset, sum = 0.0f, rounded = 0.0f;      // sums of the weights, and of the rounded ones
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[g][m][i] = 0.0f;
+    }
     const float c2 = a.scale_log2;
 
     // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
-    f32x16 s[KB];
-    uint32_t w[8 * KB];         // weights, bf16 pairs
-    float tile, tile_rounded;   // sums of a block's weights
-    auto key_operand = [&](const int (&base)[4], int st) __attribute__((always_inline)) {
-        const int b = st / 12, ks = st % 12;
-        return *reinterpret_cast<const bf16x8*>(smem + base[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow);
-    };
-    auto score = [&](int st, bf16x8 k) __attribute__((always_inline)) {
-        const int b = st / 12, ks = st % 12;
-        const f32x16 zero = {};
-        s[b] = mfma(k, q[ks], ks == 0 ? zero : s[b]);
+    f32x16 s[KB][G];
+    uint32_t w[G][8 * KB];                  // weights, bf16 pairs
+    float block_sum[G], block_rounded[G];
+    auto hide = [&](int b, int g, int key) __attribute__((always_inline)) {
+        const int here = sees(r0 + 32 * g + col) - key - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (32 * b + (i & 3) + 8 * (i >> 2) >= here) s[b][g][i] = -INFINITY;
     };
     // weights of registers 2j, 2j + 1 of block b on the present reference
-    auto weigh = [&](int b, int j) __attribute__((always_inline)) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * j], c2, -ref));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * j + 1], c2, -ref));
+    auto weigh = [&](int b, int g, int j) __attribute__((always_inline)) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][g][2 * j], c2, -ref[g]));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][g][2 * j + 1], c2, -ref[g]));
         const uint32_t pair = kc::pack_bf16x2(e0, e1);
-        w[8 * b + j] = pair;
-        tile = j == 0 ? e0 : tile + e0;
-        tile += e1;
-        tile_rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
-                                                       j == 0 ? 0.0f : tile_rounded, false);
+        w[g][8 * b + j] = pair;
+        block_sum[g] = j == 0 ? e0 : block_sum[g] + e0;
+        block_sum[g] += e1;
+        block_rounded[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
+                                                           j == 0 ? 0.0f : block_rounded[g], false);
         // (computed here: the compiler would sink it behind the next branch)
-        asm volatile("" : "+v"(w[8 * b + j]), "+v"(tile), "+v"(tile_rounded));
+        asm volatile("" : "+v"(w[g][8 * b + j]), "+v"(block_sum[g]), "+v"(block_rounded[g]));
     };
-    auto weights = [&](int ks) __attribute__((always_inline)) {
-        const u32x4 x = {w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3]};
+    auto weights = [&](int g, int ks) __attribute__((always_inline)) {
+        const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
         return __builtin_bit_cast(bf16x8, x);
     };
-    auto too_large = [&]() __attribute__((always_inline)) { return __ballot(!(tile < kMost)) != 0; };
+    auto too_large = [&]() __attribute__((always_inline)) {
+        float most = block_sum[0];
+        if constexpr (G == 2) most += block_sum[1];
+        return __ballot(!(most < kMost)) != 0;
+    };
+    auto take_sums = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            sum[g] += block_sum[g];
+            rounded[g] += block_rounded[g];
+        }
+    };
 
-    // Any tile (its operands at kt, vt), from block `from` on: the causal limit, the
-    // range's end, references that move.
+    // Any tile, from block `from` on: references that are not set or have to move,
+    // values that are not finite.
     auto any_tile = [&](int key, int off, int from) __attribute__((always_inline)) {
         const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
         const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
-        const int seen_here = seen - key - 4 * half;
-        // a key that some row does not see must not reach that row through 0 * inf
-        // or 0 * NaN: values that are not finite are left out of the product, and
-        // added to the rows that see them (to which they give what they are)
-        uint32_t found = 0;
-        if (key + KT > see_first) {
-#pragma unroll
-            for (int i = 0; i < 2 * S::plane / 1024; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4*>(smem + off + S::value_at + i * 1024 + lane * 16);
-                const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // an exponent of all ones carries
-            }
-        }
-        const bool odd = __ballot(found != 0) != 0;
+        const bool odd = key + KT > see_block && odd_values(off);
         auto block = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-            for (int ks = 0; ks < 12; ++ks) score(12 * b + ks, key_operand(kt, 12 * b + ks));
+            for (int ks = 0; ks < 12; ++ks) {
+                const bf16x8 k = key_operand(kt, 12 * b + ks);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (32 * b + (i & 3) + 8 * (i >> 2) >= seen_here) s[b][i] = -INFINITY;
-            float top = s[b][0];
+                for (int g = 0; g < G; ++g) score_mfma(s[b][g], k, q[g][ks], ks == 0);
+            }
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            top = max_halves(top) * c2;
-            if (__ballot(top > ref) != 0) {
-                const float next = fminf(fmaxf(ref, top), FLT_MAX);     // (a score of +inf: weight, sum and lse +inf)
-                const float f = __builtin_amdgcn_exp2f(ref - next);
-                ref = next;
-                sum *= f;
-                rounded *= f;
+            for (int g = 0; g < G; ++g) {
+                scores_ready(s[b][g]);
+                hide(b, g, key);
+                float top = s[b][g][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][g][i]);
+                top = max_halves(top) * c2;
+                const float next = fminf(fmaxf(ref[g], top), FLT_MAX);      // (a score of +inf: weight, sum and lse +inf)
+                const float f = __builtin_amdgcn_exp2f(ref[g] - next);
+                ref[g] = next;
+                if (__ballot(f != 1.0f && sum[g] != 0.0f) != 0) {
+                    sum[g] *= f;
+                    rounded[g] *= f;
+                    acc_wait(acc[g]);
+                    acc_scale(acc[g], f);
+                    acc_wait(acc[g]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) weigh(b, g, j);
+            }
+            take_sums();
+            if (!odd) {
+#pragma unroll
+                for (int st = 8 * b; st < 8 * b + 8; ++st) {
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, value_operand(vt, st));
+#pragma unroll
+                    for (int g = 0; g < G; ++g) acc[g][st & 3] = mfma(v, weights(g, st >> 2), acc[g][st & 3]);
+                }
+                return;
+            }
+            // values that are not finite are left out of the product, and added to the
+            // rows that see them (to which they give what they are)
+#pragma unroll
+            for (int st = 8 * b; st < 8 * b + 8; ++st) {
+                auto v = value_operand(vt, st);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = (v[j] & 0x7F80) == 0x7F80 ? 0 : v[j];
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g][st & 3] = mfma(__builtin_bit_cast(bf16x8, v), weights(g, st >> 2), acc[g][st & 3]);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) acc_wait(acc[g]);
+#pragma unroll 1
+            for (int j = 32 * b; j < 32 * b + 32; ++j) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+                    for (int i = 0; i < 16; ++i) {
+                        const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
+                        const uint32_t bits = *reinterpret_cast<const uint16_t*>(
+                            smem + off + S::value_at + (m >> 1) * S::plane + j * kRow + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
+                        const float x = (bits & 0x7F80u) == 0x7F80u ? __uint_as_float(bits << 16) : 0.0f;
+#pragma unroll
+                        for (int g = 0; g < G; ++g) acc_add(acc[g][m], i, key + j < sees(r0 + 32 * g + col) ? x : 0.0f);
+                    }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) weigh(b, j);
-            sum += tile;
-            rounded += tile_rounded;
-#pragma unroll
-            for (int st = 8 * b; st < 8 * b + 8; ++st) {
-                auto v8 = value_operand(vt, st >> 2, st & 3);
-                if (odd) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if ((v8[j] & 0x7F80) == 0x7F80) v8[j] = 0;
-                }
-                acc[st & 3] = mfma(__builtin_bit_cast(bf16x8, v8), weights(st >> 2), acc[st & 3]);
-            }
+            for (int g = 0; g < G; ++g) acc_wait(acc[g]);
         };
         if (from == 0) block(0);
         if constexpr (KB == 2) block(1);
-        if (!odd) return;
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll 1
-            for (int j = 32 * from; j < KT; ++j) {
-                const uint8_t* row = smem + off + S::value_at + (m >> 1) * S::plane + j * kRow;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
-                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(row + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
-                    if ((bits & 0x7F80u) == 0x7F80u && key + j < seen) acc[m][i] += __uint_as_float(bits << 16);
-                }
-            }
     };
 
-    // The loads of a whole tile: a wave's are a swizzle period (16 rows) apart, or
-    // half of one, so a lane has two offsets per kind of row, and the rest is scalar.
-    const int x0 = wave * 8 + (lane >> 3);
-    const uint32_t c0 = ((lane & 7) ^ score_xor(x0)) * 16;
-    const uint32_t at_n[2] = {x0 * kn_b + c0, x0 * kn_b + (c0 ^ 64)}, at_r[2] = {x0 * kr_b + c0, x0 * kr_b + (c0 ^ 64)};
-    const uint32_t at_v = x0 * vv_b + ((lane & 7) ^ value_xor(x0)) * 16;
-    auto load_whole = [&](int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v) __attribute__((always_inline)) {
-        const int plane = i * NW / S::blocks, first = i * NW % S::blocks;
-        const uint32_t at = lds0 + to + plane * S::plane + (first + wave) * 1024;
-        if (plane < 2) kc::dma16_m0(n + plane * kRow + static_cast<uint64_t>(first * 8) * kn_b, at_n[first & 1], at);
-        else if (plane == 2) kc::dma16_m0(r + static_cast<uint64_t>(first * 8) * kr_b, at_r[first & 1], at);
-        else kc::dma16_m0(v + (plane - 3) * kRow + static_cast<uint64_t>(first * 8) * vv_b, at_v, at);
-    };
-
-    // One tile by any_tile, then as many as there are that every row sees whole, with
-    // another whole tile behind them, until one's weights are too large for a
-    // reference: that one goes to any_tile again, from its block on.
+    // The usual tile: the references hold, the values are finite.  Returns the block
+    // from which any_tile has to do it over (the wave has not met the others yet), or
+    // KB when it is done.
     //
     // A slot is one matrix instruction and what is issued in its shadow: the operand
-    // read of a later slot, a load of the next tile, a piece of the softmax.  The
-    // scheduling barriers keep that order.  (Moving the reference here would make the
-    // compiler copy the accumulators in every tile.)
-    const int whole = min(see_first, key1 - KT);        // (see_first: keys that the block's first row sees)
-    int key = key0, off = 0, from = 0;
-    bool entered = false;
-    while (key < key1) {
-        if (!entered) {
-            tile_barrier();         // this tile is in LDS; every wave is done with the other buffer
-            if (key + KT < key1) stage(key + KT, S::tile - off);
-        }
-        if (key < see_max) any_tile(key, off, from);    // (else no row of this wave sees any of it)
-        entered = false;
-        from = 0;
-        key += KT;
-        off = S::tile - off;
-
-        constexpr int kScores = 12 * KB, kValues = 8 * KB, kAhead = 4;
-        static_assert(S::loads <= kScores || NW == 1, "loads of the next tile in the score slots");
-        while (key + KT <= whole) {
-            tile_barrier();
-            const uint32_t to = S::tile - off;
-            const uint8_t* const next_n = kn + static_cast<int64_t>(key + KT) * kn_b;
-            const uint8_t* const next_r = kr + static_cast<int64_t>(key + KT) * kr_b;
-            const uint8_t* const next_v = vv + static_cast<int64_t>(key + KT) * vv_b;
-            const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
-            const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
-            bf16x8 k[kAhead];
-            i16x8 v[kAhead];
+    // read of a later slot, a load of the tile after the next, a piece of the softmax.
+    // The scheduling barriers keep that order.  (Moving the reference here would make
+    // the compiler copy the accumulators in every tile.)
+    //
+    // kPart: tiles that some row of the wave does not see whole; they stage as any_tile
+    // does and met the others already.
+    constexpr int kScores = 12 * KB, kValues = 8 * KB, kAhead = 4;
+    bf16x8 k[kAhead];
+    auto first_operands = [&](int off) __attribute__((always_inline)) {
+        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) k[j] = key_operand(kt, j);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < kAhead; ++j) k[j] = key_operand(kt, j);
+    };
+    auto usual_tile = [&](int key, int off, auto part_of) __attribute__((always_inline)) {
+        constexpr bool kPart = decltype(part_of)::value;
+        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
+        const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
+        i16x8 v[kAhead];
+        // pieces of block b's softmax: the scores' wait and mask, then the weights
+        auto softmax = [&](int b, int piece) __attribute__((always_inline)) {
+            if (piece < 0 || piece >= 8 * G) return;
+            const int g = piece / 8, j = piece % 8;
+            if (j == 0) {
+                scores_ready(s[b][g]);
+                if constexpr (kPart) hide(b, g, key);
+            }
+            weigh(b, g, j);
+        };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int st = 0; st < kScores; ++st) {
-                score(st, k[st % kAhead]);
-                if (st + kAhead < kScores) k[st % kAhead] = key_operand(kt, st + kAhead);
-                else v[st + kAhead - kScores] = value_operand(vt, 0, st + kAhead - kScores);
+        for (int st = 0; st < kScores; ++st) {
+            const bf16x8 op = k[st % kAhead];
 #pragma unroll
-                for (int i = st; i < S::loads; i += kScores) load_whole(i, to, next_n, next_r, next_v);
-                if (KB == 2 && st >= 14 && st < 22) weigh(0, st - 14);
+            for (int g = 0; g < G; ++g) {
+                score_mfma(s[st / 12][g], op, q[g][st % 12], st % 12 == 0);
+                if (g == 0) {
+                    if (st + kAhead < kScores) k[st % kAhead] = key_operand(kt, st + kAhead);
+                    else v[st + kAhead - kScores] = value_operand(vt, st + kAhead - kScores);
+                }
+                if (KB == 2 && st >= 14) softmax(0, (st - 14) * G + g);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (KB == 1) {
+        }
+        if constexpr (KB == 1) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) weigh(0, j);
-            }
-            entered = too_large();
-            if (entered) break;
-            sum += tile;
-            rounded += tile_rounded;
-            __builtin_amdgcn_sched_barrier(0);
-            auto values = [&](int b) __attribute__((always_inline)) {
+            for (int i = 0; i < 8 * G; ++i) softmax(0, i);
+        }
+        if (too_large()) return 0;
+        take_sums();
+        __builtin_amdgcn_sched_barrier(0);
+        auto values = [&](int b, auto between) __attribute__((always_inline)) {
 #pragma unroll
-                for (int st = 8 * b; st < 8 * b + 8; ++st) {
-                    const int m = st & 3;
-                    acc[m] = mfma(__builtin_bit_cast(bf16x8, v[st % kAhead]), weights(st >> 2), acc[m]);
-                    if (st + kAhead < kValues) v[st % kAhead] = value_operand(vt, (st + kAhead) >> 2, m);
-                    if (b + 1 < KB && st > 0) weigh(b + 1, st - 1);
+            for (int st = 8 * b; st < 8 * b + 8; ++st) {
+                const bf16x8 op = __builtin_bit_cast(bf16x8, v[st % kAhead]);
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    acc[g][st & 3] = mfma(op, weights(g, st >> 2), acc[g][st & 3]);
+                    if (g == 0 && st + kAhead < kValues) v[st % kAhead] = value_operand(vt, st + kAhead);
+                    between((st - 8 * b) * G + g);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            };
-            values(0);
-            if constexpr (KB == 2) {
-                weigh(1, 7);
-                if (too_large()) {
-                    entered = true;
-                    from = 1;
+            }
+        };
+        // the others are met before the last block's values; the next operands and the
+        // loads follow in its slots
+        const int ahead = after(off);
+        const uint32_t to = after(ahead);
+        const uint8_t* const next_n = kn + static_cast<int64_t>(key + 2 * KT) * kn_b;
+        const uint8_t* const next_r = kr + static_cast<int64_t>(key + 2 * KT) * kr_b;
+        const uint8_t* const next_v = vv + static_cast<int64_t>(key + 2 * KT) * vv_b;
+        int kn_t[4];
+        auto last = [&](int i) __attribute__((always_inline)) {
+            if constexpr (!kPart) {
+                constexpr int kSlots = 8 * G;
+#pragma unroll
+                for (int j = i; j < S::loads; j += kSlots) load_whole(j, to, next_n, next_r, next_v);
+                if (i >= kSlots - kAhead) k[i + kAhead - kSlots] = key_operand(kn_t, i + kAhead - kSlots);
+            }
+        };
+        if constexpr (KB == 2) {
+            values(0, [&](int i) __attribute__((always_inline)) { softmax(1, i - 1); });
+            softmax(1, 8 * G - 1);
+            if (too_large()) return 1;
+            take_sums();
+        }
+        if constexpr (!kPart) {
+            meet(key, off);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kn_t[j] = at_tile(ka[j], ahead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        values(KB - 1, last);
+        return KB;
+    };
+
+    if (key0 < key1) {
+        if (key0 + KT < key1) {
+            stage(key0 + KT, S::tile);
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(S::loads) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        }
+        look(key0, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    }
+    int key = key0, off = 0;
+    int from = 0;               // block from which any_tile takes the present tile
+    bool met = false;           // whether the wave met the others in it
+    while (key < key1) {
+        // the first tile, and those that are not, or were not, for usual_tile
+        if (!met) {
+            meet(key, off);
+            stage_ahead(key, off);
+        }
+        if (key < see_last) any_tile(key, off, from);
+        key += KT;
+        off = after(off);
+        from = 0;
+        met = false;
+        // tiles that every row of the wave sees whole, with two more whole ones behind them
+        const int whole = min(see_first, key1 - 2 * KT);
+        if (key + KT <= whole) {
+            first_operands(off);
+            do {
+                from = usual_tile(key, off, std::false_type{});
+                if (from < KB) break;
+                key += KT;
+                off = after(off);
+            } while (key + KT <= whole);
+            if (from < KB) continue;
+            from = 0;
+        }
+        // the causal limit, the range's end
+        while (key < key1) {
+            if (key + KT > see_block && odd_values(off)) break;
+            meet(key, off);
+            stage_ahead(key, off);
+            if (key < see_last) {       // (else no row of this wave sees any of it)
+                first_operands(off);
+                from = usual_tile(key, off, std::true_type{});
+                if (from < KB) {
+                    met = true;
                     break;
                 }
-                sum += tile;
-                rounded += tile_rounded;
-                __builtin_amdgcn_sched_barrier(0);
-                values(1);
+                from = 0;
             }
             key += KT;
-            off = S::tile - off;
+            off = after(off);
         }
     }
 
     // ---- results: register i of block m is channel 32 m + (i & 3) + 8 (i >> 2) + 4 half
-    sum = sum_halves(sum);
-    rounded = sum_halves(rounded);
-    if (r >= q_rows) return;
-    // weights that all vanish leave 0 here; whether that is a row without keys is
-    // decided below, by what the row sees
-    const float inv = rounded == 0.0f ? 0.0f : 1.0f / rounded;
-    if (part >= 0) {
-        const int64_t row = (static_cast<int64_t>(part) * a.H + head) * (NW * kRowsPerWave) + r;
-        float* o = a.part_o + row * kValue + 4 * half;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const float total = sum_halves(sum[g]), total_rounded = sum_halves(rounded[g]);
+        // weights that all vanish leave 0 here; whether that is a row without keys is
+        // decided below, by what the row sees
+        const float inv = total_rounded == 0.0f ? 0.0f : 1.0f / total_rounded;
+        const int r = r0 + 32 * g + col;
+        if (part >= 0) {
+            if (r >= q_rows) continue;
+            const int64_t row = (static_cast<int64_t>(part) * a.H + head) * S::rows + r;
+            float* o = a.part_o + row * kValue + 4 * half;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<float4*>(o + 32 * m + 2 * i) =
+                        make_float4(acc[g][m][i] * inv, acc[g][m][i + 1] * inv, acc[g][m][i + 2] * inv, acc[g][m][i + 3] * inv);
+            if (half == 0) {
+                a.part_m[row] = ref[g];
+                a.part_l[row] = total;
+            }
+            continue;
+        }
+        // a row that sees no key is 0 (lse -inf); one whose keys all weigh nothing is not a number
+        const bool none = sees(r) <= key0;
+        const float scale = none || total != 0.0f ? inv : NAN;
+        if (a.lse != nullptr && half == 0 && r < q_rows)
+            a.lse[(static_cast<int64_t>(q_row) + r) * a.H + head] = none ? -INFINITY : (ref[g] + log2f(total)) * 0.6931471805599453f;
+        // Through LDS, so that a store instruction writes whole rows: 32 rows of 256
+        // bytes, 16 bytes c of row x at place c ^ (x & 15).  The wave's own place in the
+        // two buffers that hold no tile any more.
+        uint8_t* const own = smem + (off + (wave * G + g) * 32 * 256) % (S::buffers * S::tile);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4*>(o + 32 * m + 2 * i) = make_float4(acc[m][i] * inv, acc[m][i + 1] * inv, acc[m][i + 2] * inv, acc[m][i + 3] * inv);
-        if (half == 0) {
-            a.part_m[row] = ref;
-            a.part_l[row] = sum;
+            for (int i = 0; i < 16; i += 4) {
+                const int c = 4 * m + (i >> 2);
+                *reinterpret_cast<uint2*>(own + col * 256 + ((c ^ (col & 15)) << 4) + 8 * half) =
+                    make_uint2(kc::pack_bf16x2(acc[g][m][i] * scale, acc[g][m][i + 1] * scale),
+                               kc::pack_bf16x2(acc[g][m][i + 2] * scale, acc[g][m][i + 3] * scale));
+            }
+        // (a wave reads back only what it wrote: LDS accesses of a wave are in order)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int x = 4 * i + (lane >> 4), c = lane & 15;
+            const uint4 y = *reinterpret_cast<const uint4*>(own + x * 256 + ((c ^ (x & 15)) << 4));
+            if (r0 + 32 * g + x < q_rows)
+                *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(q_row) + r0 + 32 * g + x) * a.out_stride_t +
+                                          static_cast<int64_t>(head) * a.out_stride_h + 8 * c) = y;
         }
-        return;
     }
-    // a row that sees no key is 0 (lse -inf); one whose keys all weigh nothing is not a number
-    const bool none = seen <= key0;
-    const float scale = none || sum != 0.0f ? inv : NAN;
-    uint16_t* o = a.out + (static_cast<int64_t>(q_row) + r) * a.out_stride_t + static_cast<int64_t>(head) * a.out_stride_h + 4 * half;
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<uint2*>(o + 32 * m + 2 * i) = make_uint2(kc::pack_bf16x2(acc[m][i] * scale, acc[m][i + 1] * scale),
-                                                                       kc::pack_bf16x2(acc[m][i + 2] * scale, acc[m][i + 3] * scale));
-    if (a.lse != nullptr && half == 0)
-        a.lse[(static_cast<int64_t>(q_row) + r) * a.H + head] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
 }
 
 // Joins a block's partials: one wave per (block, head, row), two channels a lane.
@@ -489,9 +692,11 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.num_items) * static_cast<unsigned>(a.H));
     if (a.rows == 32)
-        hipLaunchKernelGGL((prefill_kernel<1, 32>), grid, dim3(64), 0, stream, a);
+        hipLaunchKernelGGL((prefill_kernel<1, 1, 32>), grid, dim3(64), 0, stream, a);
     else if (a.rows == 128)
-        hipLaunchKernelGGL((prefill_kernel<4, 64>), grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((prefill_kernel<4, 1, 64>), grid, dim3(256), 0, stream, a);
+    else if (a.rows == 256)
+        hipLaunchKernelGGL((prefill_kernel<4, 2, 64>), grid, dim3(256), 0, stream, a);
     else
         return hipErrorInvalidValue;
     const hipError_t e = hipGetLastError();
