@@ -79,6 +79,8 @@ __device__ __forceinline__ void score_mfma(f32x16& c, bf16x8 a, bf16x8 b, bool f
     else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
 }
 __device__ __forceinline__ void scores_ready(f32x16& c) { asm volatile("s_nop 7\n\ts_nop 7" : "+v"(c)); }
+// The same after four more products (each holds the matrix unit for 32 cycles).
+__device__ __forceinline__ void scores_past(f32x16& c) { asm volatile("s_nop 4" : "+v"(c)); }
 
 // Maximum / sum of a value and its copy in lane ^ 32.
 __device__ __forceinline__ float max_halves(float v) {
@@ -142,8 +144,8 @@ template <int NW, int G, int KT>
 __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     using S = Shape<NW, G, KT>;
     constexpr int KB = S::kb;
-    __shared__ __align__(1024) uint8_t smem[S::lds];
-    volatile uint32_t* const flags = reinterpret_cast<volatile uint32_t*>(smem + S::buffers * S::tile);
+    __shared__ __align__(1024) uint8_t smem[S::buffers * S::tile];
+    __shared__ uint32_t flags[S::buffers * NW];
 
     const int lane = static_cast<int>(threadIdx.x) & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -336,18 +338,22 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         for (int i = 0; i < 16; ++i)
             if (32 * b + (i & 3) + 8 * (i >> 2) >= here) s[b][g][i] = -INFINITY;
     };
-    // weights of registers 2j, 2j + 1 of block b on the present reference
-    auto weigh = [&](int b, int g, int j) __attribute__((always_inline)) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][g][2 * j], c2, -ref[g]));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][g][2 * j + 1], c2, -ref[g]));
-        const uint32_t pair = kc::pack_bf16x2(e0, e1);
-        w[g][8 * b + j] = pair;
-        block_sum[g] = j == 0 ? e0 : block_sum[g] + e0;
-        block_sum[g] += e1;
+    // Weight of register i of block b on the present reference (in order of i: pairs
+    // are rounded together).
+    float held;
+    auto weigh = [&](int b, int g, int i) __attribute__((always_inline)) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[b][g][i], c2, -ref[g]));
+        block_sum[g] = i == 0 ? e : block_sum[g] + e;
+        if ((i & 1) == 0) {
+            held = e;
+            asm volatile("" : "+v"(held), "+v"(block_sum[g]));     // (computed here, not sunk behind the next branch)
+            return;
+        }
+        uint32_t& pair = w[g][8 * b + (i >> 1)];
+        pair = kc::pack_bf16x2(held, e);
         block_rounded[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
-                                                           j == 0 ? 0.0f : block_rounded[g], false);
-        // (computed here: the compiler would sink it behind the next branch)
-        asm volatile("" : "+v"(w[g][8 * b + j]), "+v"(block_sum[g]), "+v"(block_rounded[g]));
+                                                           i == 1 ? 0.0f : block_rounded[g], false);
+        asm volatile("" : "+v"(pair), "+v"(block_sum[g]), "+v"(block_rounded[g]));
     };
     auto weights = [&](int g, int ks) __attribute__((always_inline)) {
         const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
@@ -398,7 +404,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
                     acc_wait(acc[g]);
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) weigh(b, g, j);
+                for (int i = 0; i < 16; ++i) weigh(b, g, i);
             }
             take_sums();
             if (!odd) {
@@ -443,104 +449,206 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         if constexpr (KB == 2) block(1);
     };
 
-    // The usual tile: the references hold, the values are finite.  Returns the block
-    // from which any_tile has to do it over (the wave has not met the others yet), or
-    // KB when it is done.
+    // The usual tile: the references hold, the values are finite.  Its products are
+    //   A  scores of block 0        B  scores of block 1
+    //   C  values of block 0        D  values of block 1
+    // and block 0's softmax lies between A and C, block 1's between B and D.  From tile
+    // to tile they run in the order  B(j) C(j) A(j+1) D(j): either softmax then has a
+    // score and a value phase to spread over.
     //
-    // A slot is one matrix instruction and what is issued in its shadow: the operand
-    // read of a later slot, a load of the tile after the next, a piece of the softmax.
-    // The scheduling barriers keep that order.  (Moving the reference here would make
-    // the compiler copy the accumulators in every tile.)
-    //
-    // kPart: tiles that some row of the wave does not see whole; they stage as any_tile
-    // does and met the others already.
-    constexpr int kScores = 12 * KB, kValues = 8 * KB, kAhead = 4;
-    bf16x8 k[kAhead];
-    auto first_operands = [&](int off) __attribute__((always_inline)) {
-        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
+    // A slot is one matrix instruction and what is issued in its shadow: at most one
+    // weight, the operand read of a later slot, a load of the tile after the next.  The
+    // scheduling barriers keep that order.  (Moving the reference here would make the
+    // compiler copy the accumulators in every tile.)
+    constexpr int kAhead = 4, kWeights = 16 * G;
+    constexpr int kUnits = kWeights + 3, kEarly = G == 2 ? 12 : 8;      // of them in the value phase
+    bf16x8 ring[kAhead];                        // operands on their way from LDS
+    int kt[4], vt[2];                           // the tile's operand addresses
+    auto set_tile = [&](int off) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) k[j] = key_operand(kt, j);
+        for (int j = 0; j < 4; ++j) kt[j] = at_tile(ka[j], off);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], off);
     };
-    auto usual_tile = [&](int key, int off, auto part_of) __attribute__((always_inline)) {
-        constexpr bool kPart = decltype(part_of)::value;
-        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
-        const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
-        i16x8 v[kAhead];
-        // pieces of block b's softmax: the scores' wait and mask, then the weights
-        auto softmax = [&](int b, int piece) __attribute__((always_inline)) {
-            if (piece < 0 || piece >= 8 * G) return;
-            const int g = piece / 8, j = piece % 8;
-            if (j == 0) {
-                scores_ready(s[b][g]);
-                if constexpr (kPart) hide(b, g, key);
-            }
-            weigh(b, g, j);
-        };
-        __builtin_amdgcn_sched_barrier(0);
+    auto nothing = [](int) __attribute__((always_inline)) {};
+    // Slots of block b's scores / values; ahead(f) reads operand f from the phase's start
+    // that lies behind it; more(slot) goes with the slot.
+    auto score_phase = [&](int b, auto ahead, auto more) __attribute__((always_inline)) {
 #pragma unroll
-        for (int st = 0; st < kScores; ++st) {
-            const bf16x8 op = k[st % kAhead];
+        for (int f = 0; f < 12; ++f) {
+            const bf16x8 op = ring[f % kAhead];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                score_mfma(s[st / 12][g], op, q[g][st % 12], st % 12 == 0);
-                if (g == 0) {
-                    if (st + kAhead < kScores) k[st % kAhead] = key_operand(kt, st + kAhead);
-                    else v[st + kAhead - kScores] = value_operand(vt, st + kAhead - kScores);
-                }
-                if (KB == 2 && st >= 14) softmax(0, (st - 14) * G + g);
+                score_mfma(s[b][g], op, q[g][f], f == 0);
+                if (g == 0) ring[f % kAhead] = f + kAhead < 12 ? key_operand(kt, 12 * b + f + kAhead) : ahead(f + kAhead - 12);
+                more(f * G + g);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if constexpr (KB == 1) {
+    };
+    auto value_phase = [&](int b, auto ahead, auto more) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8 * G; ++i) softmax(0, i);
+        for (int f = 0; f < 8; ++f) {
+            const bf16x8 op = ring[f % kAhead];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                acc[g][f & 3] = mfma(op, weights(g, 2 * b + (f >> 2)), acc[g][f & 3]);
+                if (g == 0)
+                    ring[f % kAhead] = f + kAhead < 8 ? __builtin_bit_cast(bf16x8, value_operand(vt, 8 * b + f + kAhead)) : ahead(f + kAhead - 8);
+                more(f * G + g);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        if (too_large()) return 0;
-        take_sums();
+    };
+    auto keys_of = [&](int b) __attribute__((always_inline)) { return [&, b](int f) __attribute__((always_inline)) { return key_operand(kt, 12 * b + f); }; };
+    auto values_of = [&](int b) __attribute__((always_inline)) { return [&, b](int f) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, value_operand(vt, 8 * b + f)); }; };
+    auto keep = [&](int f) __attribute__((always_inline)) { return ring[f]; };
+    // The softmax of block b, in units: the argument of weight u, the exponential of
+    // weight u - 1, the sum (and rounding) of weight u - 2, so that no instruction of a
+    // unit waits for another (a wave alone on its SIMD would stand still for it).  The
+    // early units start in slot 4 of the value phase (4 products after the scores), the
+    // late ones, and the test of the sums, fill the score phase.
+    float argument, weight, kept;               // in the units' pipeline
+    auto unit = [&](int b, int u) __attribute__((always_inline)) {
+        if (u >= 2 && u - 2 < kWeights) {
+            const int g = (u - 2) / 16, i = (u - 2) % 16;
+            block_sum[g] = i == 0 ? weight : block_sum[g] + weight;
+            if (i & 1) w[g][8 * b + (i >> 1)] = kc::pack_bf16x2(kept, weight);
+            else kept = weight;
+            asm volatile("" : "+v"(block_sum[g]));      // (computed here, not sunk behind the next branch)
+            if (i & 1) asm volatile("" : "+v"(w[g][8 * b + (i >> 1)]));
+        }
+        if (u >= 4 && (u & 1) == 0) {
+            const int g = (u - 4) / 16, i = (u - 4) % 16;      // the pair i, i + 1 was rounded in the unit before
+            block_rounded[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[g][8 * b + (i >> 1)]),
+                                                               __builtin_bit_cast(bf16x2, 0x3F803F80u), i == 0 ? 0.0f : block_rounded[g], false);
+            asm volatile("" : "+v"(block_rounded[g]));
+        }
+        if (u >= 1 && u - 1 < kWeights) {
+            weight = __builtin_amdgcn_exp2f(argument);
+            asm volatile("" : "+v"(weight));
+        }
+        if (u < kWeights) {
+            argument = fmaf(s[b][u / 16][u % 16], c2, -ref[u / 16]);
+            asm volatile("" : "+v"(argument));
+        }
+    };
+    auto early = [&](int b, int slot) __attribute__((always_inline)) {
+        if (slot < 4) return;
+        if (slot == 4) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) scores_past(s[b][g]);
+        }
+        constexpr int per = kEarly / (8 * G - 4);
+#pragma unroll
+        for (int u = 0; u < per; ++u) unit(b, (slot - 4) * per + u);
+    };
+    bool over = false;
+    auto late = [&](int b, int slot) __attribute__((always_inline)) {
+        if (kEarly + slot < kUnits) unit(b, kEarly + slot);
+        else if (slot == 12 * G - 1) over = too_large();
+    };
+    static_assert(kUnits - kEarly == 12 * G - 1, "the last slot tests the sums");
+    auto weigh_rest = [&](int b, int from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (u >= from) unit(b, u);
+        over = too_large();
+    };
+    const uint8_t *next_n, *next_r, *next_v;    // rows of the tile after the next
+    // A of a tile by itself, and its block's early weights (hidden: of a tile that some
+    // row of the wave does not see whole); ends with B's (or C's) operands on their way.
+    auto begin_tile = [&](int key, int off, bool hidden) __attribute__((always_inline)) {
+        set_tile(off);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ring[j] = key_operand(kt, j);
         __builtin_amdgcn_sched_barrier(0);
-        auto values = [&](int b, auto between) __attribute__((always_inline)) {
+        if constexpr (KB == 2) score_phase(0, keys_of(1), nothing);
+        else score_phase(0, values_of(0), nothing);
 #pragma unroll
-            for (int st = 8 * b; st < 8 * b + 8; ++st) {
-                const bf16x8 op = __builtin_bit_cast(bf16x8, v[st % kAhead]);
+        for (int g = 0; g < G; ++g) {
+            scores_ready(s[0][g]);
+            if (hidden) hide(0, g, key);
+        }
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    acc[g][st & 3] = mfma(op, weights(g, st >> 2), acc[g][st & 3]);
-                    if (g == 0 && st + kAhead < kValues) v[st % kAhead] = value_operand(vt, st + kAhead);
-                    between((st - 8 * b) * G + g);
-                    __builtin_amdgcn_sched_barrier(0);
+        for (int u = 0; u < kEarly; ++u) unit(0, u);
+    };
+    // The rest of a tile after begin_tile; kNext: with the next tile's A and early
+    // weights (whole, and another whole tile behind it), else by itself, the mask on
+    // block 1.  Returns the block from which any_tile has to take the tile, or KB.
+    auto finish_tile = [&](int key, int off, auto with_next) __attribute__((always_inline)) {
+        constexpr bool kNext = decltype(with_next)::value;
+        const int next = after(off);
+        const uint32_t to = after(next);
+        meet(key, off);
+        if constexpr (!kNext) stage_ahead(key, off);
+        // (spread over the 20 G slots of B and C)
+        auto load_slot = [&](int slot) __attribute__((always_inline)) {
+            if constexpr (kNext) {
+#pragma unroll
+                for (int i = 0; i < S::loads; ++i)
+                    if (i * 20 * G / S::loads == slot) load_whole(i, to, next_n, next_r, next_v);
+            }
+        };
+        int done = 0;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (KB == 1) {
+            weigh_rest(0, kEarly);
+            if (!over) {
+                take_sums();
+                value_phase(0, keep, nothing);
+                done = 1;
+            }
+        } else {
+            score_phase(1, values_of(0), [&](int slot) __attribute__((always_inline)) {
+                late(0, slot);
+                load_slot(slot);
+            });
+            if (__builtin_expect(over, 0)) {
+#pragma unroll
+                for (int slot = 12 * G; slot < 20 * G; ++slot) load_slot(slot);
+            } else {
+                take_sums();
+                done = 1;
+                if constexpr (kNext) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) kt[j] = at_tile(ka[j], next);
+                    value_phase(0, keys_of(0), [&](int slot) __attribute__((always_inline)) {
+                        early(1, slot);
+                        load_slot(12 * G + slot);
+                    });
+                    score_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { late(1, slot); });
+                    if (__builtin_expect(!over, 1)) {
+                        take_sums();
+                        done = 2;
+                        value_phase(1, keys_of(1), [&](int slot) __attribute__((always_inline)) {
+                            early(0, slot);
+                            if (slot == 0) {
+                                next_n += static_cast<uint64_t>(KT) * kn_b;
+                                next_r += static_cast<uint64_t>(KT) * kr_b;
+                                next_v += static_cast<uint64_t>(KT) * vv_b;
+                            }
+                        });
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], next);
+                    }
+                } else {
+                    value_phase(0, values_of(1), nothing);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        scores_ready(s[1][g]);
+                        hide(1, g, key);
+                    }
+                    weigh_rest(1, 0);
+                    if (!over) {
+                        take_sums();
+                        done = 2;
+                        value_phase(1, keep, nothing);
+                    }
                 }
             }
-        };
-        // the others are met before the last block's values; the next operands and the
-        // loads follow in its slots
-        const int ahead = after(off);
-        const uint32_t to = after(ahead);
-        const uint8_t* const next_n = kn + static_cast<int64_t>(key + 2 * KT) * kn_b;
-        const uint8_t* const next_r = kr + static_cast<int64_t>(key + 2 * KT) * kr_b;
-        const uint8_t* const next_v = vv + static_cast<int64_t>(key + 2 * KT) * vv_b;
-        int kn_t[4];
-        auto last = [&](int i) __attribute__((always_inline)) {
-            if constexpr (!kPart) {
-                constexpr int kSlots = 8 * G;
-#pragma unroll
-                for (int j = i; j < S::loads; j += kSlots) load_whole(j, to, next_n, next_r, next_v);
-                if (i >= kSlots - kAhead) k[i + kAhead - kSlots] = key_operand(kn_t, i + kAhead - kSlots);
-            }
-        };
-        if constexpr (KB == 2) {
-            values(0, [&](int i) __attribute__((always_inline)) { softmax(1, i - 1); });
-            softmax(1, 8 * G - 1);
-            if (too_large()) return 1;
-            take_sums();
         }
-        if constexpr (!kPart) {
-            meet(key, off);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) kn_t[j] = at_tile(ka[j], ahead);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        values(KB - 1, last);
-        return KB;
+        return done;
     };
 
     if (key0 < key1) {
@@ -567,32 +675,38 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         off = after(off);
         from = 0;
         met = false;
-        // tiles that every row of the wave sees whole, with two more whole ones behind them
-        const int whole = min(see_first, key1 - 2 * KT);
-        if (key + KT <= whole) {
-            first_operands(off);
+        // tiles that every row of the wave sees whole, as the next one, with another whole
+        // one behind that
+        const int last_followed = min(see_first - 2 * KT, key1 - 3 * KT);
+        if (KB == 2 && key <= last_followed) {
+            begin_tile(key, off, false);
+            next_n = kn + static_cast<int64_t>(key + 2 * KT) * kn_b;
+            next_r = kr + static_cast<int64_t>(key + 2 * KT) * kr_b;
+            next_v = vv + static_cast<int64_t>(key + 2 * KT) * vv_b;
             do {
-                from = usual_tile(key, off, std::false_type{});
-                if (from < KB) break;
-                key += KT;
-                off = after(off);
-            } while (key + KT <= whole);
-            if (from < KB) continue;
+                from = finish_tile(key, off, std::true_type{});
+                key += from == KB ? KT : 0;
+                off = from == KB ? after(off) : off;
+            } while (from == KB && key <= last_followed);
+            if (from == KB) from = finish_tile(key, off, std::false_type{});
+            met = from < KB;
+            if (met) continue;
+            key += KT;
+            off = after(off);
             from = 0;
         }
         // the causal limit, the range's end
         while (key < key1) {
             if (key + KT > see_block && odd_values(off)) break;
-            meet(key, off);
-            stage_ahead(key, off);
-            if (key < see_last) {       // (else no row of this wave sees any of it)
-                first_operands(off);
-                from = usual_tile(key, off, std::true_type{});
-                if (from < KB) {
-                    met = true;
-                    break;
-                }
+            if (key < see_last) {
+                begin_tile(key, off, true);
+                from = finish_tile(key, off, std::false_type{});
+                met = from < KB;
+                if (met) break;
                 from = 0;
+            } else {            // no row of this wave sees any of it
+                meet(key, off);
+                stage_ahead(key, off);
             }
             key += KT;
             off = after(off);
