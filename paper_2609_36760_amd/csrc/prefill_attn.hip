@@ -28,10 +28,12 @@
 // block runs between the products of the next.
 //
 // Roundings: the weights are bf16 operands of the second product (at most 2^-8
-// of a weight, as the bf16 output's own rounding).  The output is normalized by
-// the sum of the rounded weights, so that a row that one key dominates is not
-// scaled by that key's rounding; lse takes the sum of the fp32 weights.
-// Scores, reference, sums and accumulators are fp32.
+// of a weight, as the bf16 output's own rounding; bf16 values allow no wider
+// ones).  Scores, reference, sum and accumulators are fp32, the sum taken of the
+// weights before their rounding.  (Normalizing by the sum of the rounded weights
+// would spare rows that one key dominates that key's rounding, but bf16 dot
+// products take the matrix unit's time, 11 cycles each, and unpacking the weights
+// four more vector instructions a pair.)
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
 // any reference that keeps them far from overflow: a row's is its maximum over
@@ -57,7 +59,6 @@ using kc::f32x16;
 using kc::i16x4;
 using kc::lds_i16x4;
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -316,11 +317,11 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     };
 
     f32x16 acc[G][4];
-    float ref[G], sum[G], rounded[G];       // reference; sums of the weights, and of the rounded ones
+    float ref[G], sum[G];                   // reference, sum of the weights
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         ref[g] = kUnset;
-        sum[g] = rounded[g] = 0.0f;
+        sum[g] = 0.0f;
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
     f32x16 s[KB][G];
     uint32_t w[G][8 * KB];                  // weights, bf16 pairs
-    float block_sum[G], block_rounded[G];
+    float block_sum[G];
     auto hide = [&](int b, int g, int key) __attribute__((always_inline)) {
         const int here = sees(r0 + 32 * g + col) - key - 4 * half;
 #pragma unroll
@@ -344,16 +345,8 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     auto weigh = [&](int b, int g, int i) __attribute__((always_inline)) {
         const float e = __builtin_amdgcn_exp2f(fmaf(s[b][g][i], c2, -ref[g]));
         block_sum[g] = i == 0 ? e : block_sum[g] + e;
-        if ((i & 1) == 0) {
-            held = e;
-            asm volatile("" : "+v"(held), "+v"(block_sum[g]));     // (computed here, not sunk behind the next branch)
-            return;
-        }
-        uint32_t& pair = w[g][8 * b + (i >> 1)];
-        pair = kc::pack_bf16x2(held, e);
-        block_rounded[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u),
-                                                           i == 1 ? 0.0f : block_rounded[g], false);
-        asm volatile("" : "+v"(pair), "+v"(block_sum[g]), "+v"(block_rounded[g]));
+        if (i & 1) w[g][8 * b + (i >> 1)] = kc::pack_bf16x2(held, e);
+        else held = e;
     };
     auto weights = [&](int g, int ks) __attribute__((always_inline)) {
         const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
@@ -366,10 +359,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     };
     auto take_sums = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            sum[g] += block_sum[g];
-            rounded[g] += block_rounded[g];
-        }
+        for (int g = 0; g < G; ++g) sum[g] += block_sum[g];
     };
 
     // Any tile, from block `from` on: references that are not set or have to move,
@@ -398,7 +388,6 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
                 ref[g] = next;
                 if (__ballot(f != 1.0f && sum[g] != 0.0f) != 0) {
                     sum[g] *= f;
-                    rounded[g] *= f;
                     acc_wait(acc[g]);
                     acc_scale(acc[g], f);
                     acc_wait(acc[g]);
@@ -461,7 +450,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     // scheduling barriers keep that order.  (Moving the reference here would make the
     // compiler copy the accumulators in every tile.)
     constexpr int kAhead = 4, kWeights = 16 * G;
-    constexpr int kUnits = kWeights + 3, kEarly = G == 2 ? 12 : 8;      // of them in the value phase
+    constexpr int kUnits = kWeights + 2, kEarly = G == 2 ? 12 : 8;      // of them in the value phase
     bf16x8 ring[kAhead];                        // operands on their way from LDS
     int kt[4], vt[2];                           // the tile's operand addresses
     auto set_tile = [&](int off) __attribute__((always_inline)) {
@@ -518,12 +507,6 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
             asm volatile("" : "+v"(block_sum[g]));      // (computed here, not sunk behind the next branch)
             if (i & 1) asm volatile("" : "+v"(w[g][8 * b + (i >> 1)]));
         }
-        if (u >= 4 && (u & 1) == 0) {
-            const int g = (u - 4) / 16, i = (u - 4) % 16;      // the pair i, i + 1 was rounded in the unit before
-            block_rounded[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[g][8 * b + (i >> 1)]),
-                                                               __builtin_bit_cast(bf16x2, 0x3F803F80u), i == 0 ? 0.0f : block_rounded[g], false);
-            asm volatile("" : "+v"(block_rounded[g]));
-        }
         if (u >= 1 && u - 1 < kWeights) {
             weight = __builtin_amdgcn_exp2f(argument);
             asm volatile("" : "+v"(weight));
@@ -548,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         if (kEarly + slot < kUnits) unit(b, kEarly + slot);
         else if (slot == 12 * G - 1) over = too_large();
     };
-    static_assert(kUnits - kEarly == 12 * G - 1, "the last slot tests the sums");
+    static_assert(kUnits - kEarly < 12 * G, "the last slot tests the sums");
     auto weigh_rest = [&](int b, int from) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
@@ -716,10 +699,10 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     // ---- results: register i of block m is channel 32 m + (i & 3) + 8 (i >> 2) + 4 half
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        const float total = sum_halves(sum[g]), total_rounded = sum_halves(rounded[g]);
+        const float total = sum_halves(sum[g]);
         // weights that all vanish leave 0 here; whether that is a row without keys is
         // decided below, by what the row sees
-        const float inv = total_rounded == 0.0f ? 0.0f : 1.0f / total_rounded;
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int r = r0 + 32 * g + col;
         if (part >= 0) {
             if (r >= q_rows) continue;

@@ -81,8 +81,8 @@ class Attended:
                 else w @ val
             self.out[:, h] = torch.where(some, o, 0.0)
             self.lse[:, h] = torch.where(some, lse, -math.inf)[:, 0]
-            # weights: bf16 rounding of each against that of their sum, the scores' error (numerator and sum),
-            # exp2 and fp32 sums (some 2^-20); then the output's own rounding
+            # weights: bf16 rounding of each (twice, should their sum be taken of the rounded ones), the scores' error
+            # (numerator and sum), exp2 and fp32 sums (some 2^-20); then the output's own rounding
             spread = w @ val.nan_to_num(0.0, 0.0, 0.0).abs()
             delta = 2.0 * U16 + 4.0 * dz + 2.0 ** -20 + nk * U32
             self.out_bound[:, h] = 1.01 * (U16 * self.out[:, h].nan_to_num(0.0, 0.0, 0.0).abs() + delta * spread) + 1e-30
