@@ -36,12 +36,14 @@
 // four more vector instructions a pair.)
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
-// any reference that keeps them far from overflow: a row's is its maximum over
-// its first tile, and it stays until a block's weights add up to kMost or more
-// (or to no number); then it moves to that block's maximum, the accumulators
-// follow, and the block is weighed again.  So tiles are not searched for maxima
-// as a rule.  The reference starts at the lowest finite value, on which hidden
-// scores (-inf) weigh 0.
+// any reference that keeps them from overflow: a row's is its maximum over its
+// first 32 keys, and it stays, and no later tile is searched for maxima, as long
+// as a block's weights add up to less than 2^100 -- scores 69 above the first
+// ones in natural units.  A workgroup that meets larger sums, sums that are no
+// number, or values that are not finite where a row is hidden from them, does its
+// rows over in careful_rows, which moves references tile by tile.  (Kept apart, so
+// that the accumulators have one place throughout: any other use of them between
+// the products made the compiler copy them in every tile.)
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -62,19 +64,16 @@ using kc::lds_i16x4;
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kMost = 0x1p30f;
+constexpr float kMost = 0x1p100f;
 constexpr float kUnset = -FLT_MAX;
 
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-// Score products accumulate in vector registers: kept with the output in the
-// accumulation registers, the compiler would copy every score out.  As inline
-// assembly they get no wait states: the first product of a chain writes without
-// reading, the following ones accumulate back to back (no wait between products
-// of one shape), and scores_ready supplies the wait before vector instructions
-// read the result (12 wait states after a 32 x 32 x 16 product).  The queries
-// stay in accumulation registers, beside the output.
+// Score products accumulate in vector registers, with the queries in accumulation
+// registers beside the output: kept with the output, the compiler would copy every
+// score out.  As inline assembly they get no wait states from it: the first
+// product of a chain writes without reading, the following ones accumulate back
+// to back (no wait between products of one shape), and scores_ready supplies the
+// wait before vector instructions read the result (12 wait states after a
+// 32 x 32 x 16 product).
 __device__ __forceinline__ void score_mfma(f32x16& c, bf16x8 a, bf16x8 b, bool first) {
     if (first) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
     else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
@@ -93,27 +92,8 @@ __device__ __forceinline__ float sum_halves(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Output accumulators changed outside the products: in place, in their
-// accumulation registers (as ordinary arithmetic, the compiler would move all of
-// them to vector registers and back around every use).  It places no wait states
-// around these either: acc_wait stands between products and what follows.
-__device__ __forceinline__ void acc_wait(f32x16 (&c)[4]) {
-    asm volatile("s_nop 15\n\ts_nop 7" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]));
-}
-__device__ __forceinline__ void acc_scale(f32x16 (&c)[4], float f) {
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float t;
-            asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
-                         : "+a"(c[m][i]), "=&v"(t) : "v"(f));
-        }
-}
-__device__ __forceinline__ void acc_add(f32x16& c, int i, float x) {
-    float t;
-    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_add_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
-                 : "+a"(c[i]), "=&v"(t) : "v"(x));
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
 // LDS of one tile: five planes of 64 channels (128-byte rows) of all KT keys --
@@ -137,7 +117,7 @@ struct Shape {
     static constexpr int loads = 5 * blocks / NW;           // per wave
     static_assert(blocks % NW == 0, "a wave's load belongs to one plane");
     static constexpr int buffers = 3;
-    static constexpr int lds = buffers * tile + buffers * NW * 4;
+    static constexpr int lds = buffers * tile + (buffers + 1) * NW * 4;
     static_assert(lds <= 160 * 1024 && NW * G * kRowsPerWave * 256 <= (buffers - 1) * tile, "LDS; results beside the last tile");
 };
 
@@ -146,7 +126,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     using S = Shape<NW, G, KT>;
     constexpr int KB = S::kb;
     __shared__ __align__(1024) uint8_t smem[S::buffers * S::tile];
-    __shared__ uint32_t flags[S::buffers * NW];
+    __shared__ uint32_t flags[(S::buffers + 1) * NW];
 
     const int lane = static_cast<int>(threadIdx.x) & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -328,6 +308,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
             for (int i = 0; i < 16; ++i) acc[g][m][i] = 0.0f;
     }
     const float c2 = a.scale_log2;
+    bool careful = false;                   // whether the rows have to be done over
 
     // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
     f32x16 s[KB][G];
@@ -339,106 +320,23 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         for (int i = 0; i < 16; ++i)
             if (32 * b + (i & 3) + 8 * (i >> 2) >= here) s[b][g][i] = -INFINITY;
     };
-    // Weight of register i of block b on the present reference (in order of i: pairs
-    // are rounded together).
-    float held;
-    auto weigh = [&](int b, int g, int i) __attribute__((always_inline)) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[b][g][i], c2, -ref[g]));
-        block_sum[g] = i == 0 ? e : block_sum[g] + e;
-        if (i & 1) w[g][8 * b + (i >> 1)] = kc::pack_bf16x2(held, e);
-        else held = e;
+    // the row's largest score of block b, log2 units
+    auto top_of = [&](int b, int g) __attribute__((always_inline)) {
+        float top = s[b][g][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][g][i]);
+        return max_halves(top) * c2;
     };
     auto weights = [&](int g, int ks) __attribute__((always_inline)) {
         const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
         return __builtin_bit_cast(bf16x8, x);
-    };
-    auto too_large = [&]() __attribute__((always_inline)) {
-        float most = block_sum[0];
-        if constexpr (G == 2) most += block_sum[1];
-        return __ballot(!(most < kMost)) != 0;
     };
     auto take_sums = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < G; ++g) sum[g] += block_sum[g];
     };
 
-    // Any tile, from block `from` on: references that are not set or have to move,
-    // values that are not finite.
-    auto any_tile = [&](int key, int off, int from) __attribute__((always_inline)) {
-        const int kt[4] = {at_tile(ka[0], off), at_tile(ka[1], off), at_tile(ka[2], off), at_tile(ka[3], off)};
-        const int vt[2] = {at_tile(va[0], off), at_tile(va[1], off)};
-        const bool odd = key + KT > see_block && odd_values(off);
-        auto block = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-            for (int ks = 0; ks < 12; ++ks) {
-                const bf16x8 k = key_operand(kt, 12 * b + ks);
-#pragma unroll
-                for (int g = 0; g < G; ++g) score_mfma(s[b][g], k, q[g][ks], ks == 0);
-            }
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                scores_ready(s[b][g]);
-                hide(b, g, key);
-                float top = s[b][g][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][g][i]);
-                top = max_halves(top) * c2;
-                const float next = fminf(fmaxf(ref[g], top), FLT_MAX);      // (a score of +inf: weight, sum and lse +inf)
-                const float f = __builtin_amdgcn_exp2f(ref[g] - next);
-                ref[g] = next;
-                if (__ballot(f != 1.0f && sum[g] != 0.0f) != 0) {
-                    sum[g] *= f;
-                    acc_wait(acc[g]);
-                    acc_scale(acc[g], f);
-                    acc_wait(acc[g]);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) weigh(b, g, i);
-            }
-            take_sums();
-            if (!odd) {
-#pragma unroll
-                for (int st = 8 * b; st < 8 * b + 8; ++st) {
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, value_operand(vt, st));
-#pragma unroll
-                    for (int g = 0; g < G; ++g) acc[g][st & 3] = mfma(v, weights(g, st >> 2), acc[g][st & 3]);
-                }
-                return;
-            }
-            // values that are not finite are left out of the product, and added to the
-            // rows that see them (to which they give what they are)
-#pragma unroll
-            for (int st = 8 * b; st < 8 * b + 8; ++st) {
-                auto v = value_operand(vt, st);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (v[j] & 0x7F80) == 0x7F80 ? 0 : v[j];
-#pragma unroll
-                for (int g = 0; g < G; ++g) acc[g][st & 3] = mfma(__builtin_bit_cast(bf16x8, v), weights(g, st >> 2), acc[g][st & 3]);
-            }
-#pragma unroll
-            for (int g = 0; g < G; ++g) acc_wait(acc[g]);
-#pragma unroll 1
-            for (int j = 32 * b; j < 32 * b + 32; ++j) {
-#pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
-                        const uint32_t bits = *reinterpret_cast<const uint16_t*>(
-                            smem + off + S::value_at + (m >> 1) * S::plane + j * kRow + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
-                        const float x = (bits & 0x7F80u) == 0x7F80u ? __uint_as_float(bits << 16) : 0.0f;
-#pragma unroll
-                        for (int g = 0; g < G; ++g) acc_add(acc[g][m], i, key + j < sees(r0 + 32 * g + col) ? x : 0.0f);
-                    }
-            }
-#pragma unroll
-            for (int g = 0; g < G; ++g) acc_wait(acc[g]);
-        };
-        if (from == 0) block(0);
-        if constexpr (KB == 2) block(1);
-    };
-
-    // The usual tile: the references hold, the values are finite.  Its products are
+    // A tile's products are
     //   A  scores of block 0        B  scores of block 1
     //   C  values of block 0        D  values of block 1
     // and block 0's softmax lies between A and C, block 1's between B and D.  From tile
@@ -447,8 +345,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     //
     // A slot is one matrix instruction and what is issued in its shadow: at most one
     // weight, the operand read of a later slot, a load of the tile after the next.  The
-    // scheduling barriers keep that order.  (Moving the reference here would make the
-    // compiler copy the accumulators in every tile.)
+    // scheduling barriers keep that order.
     constexpr int kAhead = 4, kWeights = 16 * G;
     constexpr int kUnits = kWeights + 2, kEarly = G == 2 ? 12 : 8;      // of them in the value phase
     bf16x8 ring[kAhead];                        // operands on their way from LDS
@@ -498,7 +395,12 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     // early units start in slot 4 of the value phase (4 products after the scores), the
     // late ones, and the test of the sums, fill the score phase.
     float argument, weight, kept;               // in the units' pipeline
-    auto unit = [&](int b, int u) __attribute__((always_inline)) {
+    int here[G];                                // keys of the tile that the lane's rows see, less 4 half
+    auto set_here = [&](int key) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) here[g] = sees(r0 + 32 * g + col) - key - 4 * half;
+    };
+    auto unit = [&](int b, int u, bool hide) __attribute__((always_inline)) {
         if (u >= 2 && u - 2 < kWeights) {
             const int g = (u - 2) / 16, i = (u - 2) % 16;
             block_sum[g] = i == 0 ? weight : block_sum[g] + weight;
@@ -512,11 +414,13 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
             asm volatile("" : "+v"(weight));
         }
         if (u < kWeights) {
-            argument = fmaf(s[b][u / 16][u % 16], c2, -ref[u / 16]);
+            const int i = u % 16;
+            argument = fmaf(s[b][u / 16][i], c2, -ref[u / 16]);
+            if (hide) argument = 32 * b + (i & 3) + 8 * (i >> 2) < here[u / 16] ? argument : -INFINITY;
             asm volatile("" : "+v"(argument));
         }
     };
-    auto early = [&](int b, int slot) __attribute__((always_inline)) {
+    auto early = [&](int b, int slot, bool hide) __attribute__((always_inline)) {
         if (slot < 4) return;
         if (slot == 4) {
 #pragma unroll
@@ -524,25 +428,25 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         }
         constexpr int per = kEarly / (8 * G - 4);
 #pragma unroll
-        for (int u = 0; u < per; ++u) unit(b, (slot - 4) * per + u);
+        for (int u = 0; u < per; ++u) unit(b, (slot - 4) * per + u, hide);
     };
-    bool over = false;
-    auto late = [&](int b, int slot) __attribute__((always_inline)) {
-        if (kEarly + slot < kUnits) unit(b, kEarly + slot);
-        else if (slot == 12 * G - 1) over = too_large();
+    auto late = [&](int b, int slot, bool hide) __attribute__((always_inline)) {
+        if (kEarly + slot < kUnits) unit(b, kEarly + slot, hide);
+        else if (slot == 12 * G - 1) take_sums();
     };
-    static_assert(kUnits - kEarly < 12 * G, "the last slot tests the sums");
-    auto weigh_rest = [&](int b, int from) __attribute__((always_inline)) {
+    static_assert(kUnits - kEarly < 12 * G, "the last slot takes the sums");
+    auto weigh_rest = [&](int b, int from, bool hide) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
-            if (u >= from) unit(b, u);
-        over = too_large();
+            if (u >= from) unit(b, u, hide);
+        take_sums();
     };
     const uint8_t *next_n, *next_r, *next_v;    // rows of the tile after the next
-    // A of a tile by itself, and its block's early weights (hidden: of a tile that some
-    // row of the wave does not see whole); ends with B's (or C's) operands on their way.
-    auto begin_tile = [&](int key, int off, bool hidden) __attribute__((always_inline)) {
+    // A of a tile by itself, and its early weights; the first tile of all sets the
+    // references.  Ends with B's (or C's) operands on their way.
+    auto begin_tile = [&](int key, int off) __attribute__((always_inline)) {
         set_tile(off);
+        set_here(key);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) ring[j] = key_operand(kt, j);
         __builtin_amdgcn_sched_barrier(0);
@@ -551,87 +455,73 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             scores_ready(s[0][g]);
-            if (hidden) hide(0, g, key);
+            if (key + KT > see_first) hide(0, g, key);
+        }
+        if (key == key0) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, top_of(0, g));      // (no key: any finite value)
         }
 #pragma unroll
-        for (int u = 0; u < kEarly; ++u) unit(0, u);
+        for (int u = 0; u < kEarly; ++u) unit(0, u, false);
     };
     // The rest of a tile after begin_tile; kNext: with the next tile's A and early
-    // weights (whole, and another whole tile behind it), else by itself, the mask on
-    // block 1.  Returns the block from which any_tile has to take the tile, or KB.
-    auto finish_tile = [&](int key, int off, auto with_next) __attribute__((always_inline)) {
-        constexpr bool kNext = decltype(with_next)::value;
+    // weights, else by itself.  kPart: some row of the wave may not see all of it (or of
+    // the next); otherwise it and the next are whole, and another whole one is behind
+    // them.  `careful` is set where the tile is not for this path.
+    auto finish_tile = [&](int key, int off, auto with_next, auto in_part) __attribute__((always_inline)) {
+        constexpr bool kNext = decltype(with_next)::value, kPart = decltype(in_part)::value;
         const int next = after(off);
         const uint32_t to = after(next);
         meet(key, off);
-        if constexpr (!kNext) stage_ahead(key, off);
+        if constexpr (kPart) {
+            stage_ahead(key, off);
+            careful = careful || (key + KT > see_block && odd_values(off));
+        }
         // (spread over the 20 G slots of B and C)
         auto load_slot = [&](int slot) __attribute__((always_inline)) {
-            if constexpr (kNext) {
+            if constexpr (!kPart) {
 #pragma unroll
                 for (int i = 0; i < S::loads; ++i)
                     if (i * 20 * G / S::loads == slot) load_whole(i, to, next_n, next_r, next_v);
             }
         };
-        int done = 0;
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (KB == 1) {
-            weigh_rest(0, kEarly);
-            if (!over) {
-                take_sums();
-                value_phase(0, keep, nothing);
-                done = 1;
-            }
+            weigh_rest(0, kEarly, kPart);
+            value_phase(0, keep, nothing);
         } else {
             score_phase(1, values_of(0), [&](int slot) __attribute__((always_inline)) {
-                late(0, slot);
+                late(0, slot, kPart);
                 load_slot(slot);
             });
-            if (__builtin_expect(over, 0)) {
+            if constexpr (kNext) {
 #pragma unroll
-                for (int slot = 12 * G; slot < 20 * G; ++slot) load_slot(slot);
-            } else {
-                take_sums();
-                done = 1;
-                if constexpr (kNext) {
+                for (int j = 0; j < 4; ++j) kt[j] = at_tile(ka[j], next);
+                value_phase(0, keys_of(0), [&](int slot) __attribute__((always_inline)) {
+                    early(1, slot, kPart);
+                    load_slot(12 * G + slot);
+                });
+                score_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { late(1, slot, kPart); });
+                if constexpr (kPart) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) kt[j] = at_tile(ka[j], next);
-                    value_phase(0, keys_of(0), [&](int slot) __attribute__((always_inline)) {
-                        early(1, slot);
-                        load_slot(12 * G + slot);
-                    });
-                    score_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { late(1, slot); });
-                    if (__builtin_expect(!over, 1)) {
-                        take_sums();
-                        done = 2;
-                        value_phase(1, keys_of(1), [&](int slot) __attribute__((always_inline)) {
-                            early(0, slot);
-                            if (slot == 0) {
-                                next_n += static_cast<uint64_t>(KT) * kn_b;
-                                next_r += static_cast<uint64_t>(KT) * kr_b;
-                                next_v += static_cast<uint64_t>(KT) * vv_b;
-                            }
-                        });
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], next);
-                    }
-                } else {
-                    value_phase(0, values_of(1), nothing);
-#pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        scores_ready(s[1][g]);
-                        hide(1, g, key);
-                    }
-                    weigh_rest(1, 0);
-                    if (!over) {
-                        take_sums();
-                        done = 2;
-                        value_phase(1, keep, nothing);
-                    }
+                    for (int g = 0; g < G; ++g) here[g] -= KT;
                 }
+                value_phase(1, keys_of(1), [&](int slot) __attribute__((always_inline)) {
+                    early(0, slot, kPart);
+                    if (!kPart && slot == 0) {
+                        next_n += static_cast<uint64_t>(KT) * kn_b;
+                        next_r += static_cast<uint64_t>(KT) * kr_b;
+                        next_v += static_cast<uint64_t>(KT) * vv_b;
+                    }
+                });
+#pragma unroll
+                for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], next);
+            } else {
+                value_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { early(1, slot, kPart); });
+                weigh_rest(1, kEarly, kPart);
+                value_phase(1, keep, nothing);
             }
         }
-        return done;
     };
 
     if (key0 < key1) {
@@ -645,108 +535,198 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
     }
     int key = key0, off = 0;
-    int from = 0;               // block from which any_tile takes the present tile
-    bool met = false;           // whether the wave met the others in it
-    while (key < key1) {
-        // the first tile, and those that are not, or were not, for usual_tile
-        if (!met) {
-            meet(key, off);
-            stage_ahead(key, off);
-        }
-        if (key < see_last) any_tile(key, off, from);
-        key += KT;
-        off = after(off);
-        from = 0;
-        met = false;
-        // tiles that every row of the wave sees whole, as the next one, with another whole
-        // one behind that
-        const int last_followed = min(see_first - 2 * KT, key1 - 3 * KT);
-        if (KB == 2 && key <= last_followed) {
-            begin_tile(key, off, false);
+    if (key < see_last) {
+        begin_tile(key, off);
+        if constexpr (KB == 2) {
+            const int last_followed = min(see_first - 2 * KT, key1 - 3 * KT);
             next_n = kn + static_cast<int64_t>(key + 2 * KT) * kn_b;
             next_r = kr + static_cast<int64_t>(key + 2 * KT) * kr_b;
             next_v = vv + static_cast<int64_t>(key + 2 * KT) * vv_b;
-            do {
-                from = finish_tile(key, off, std::true_type{});
-                key += from == KB ? KT : 0;
-                off = from == KB ? after(off) : off;
-            } while (from == KB && key <= last_followed);
-            if (from == KB) from = finish_tile(key, off, std::false_type{});
-            met = from < KB;
-            if (met) continue;
-            key += KT;
-            off = after(off);
-            from = 0;
-        }
-        // the causal limit, the range's end
-        while (key < key1) {
-            if (key + KT > see_block && odd_values(off)) break;
-            if (key < see_last) {
-                begin_tile(key, off, true);
-                from = finish_tile(key, off, std::false_type{});
-                met = from < KB;
-                if (met) break;
-                from = 0;
-            } else {            // no row of this wave sees any of it
-                meet(key, off);
-                stage_ahead(key, off);
+            while (key <= last_followed) {
+                finish_tile(key, off, std::true_type{}, std::false_type{});
+                key += KT;
+                off = after(off);
             }
-            key += KT;
-            off = after(off);
+            set_here(key);
+            while (key + KT < see_last) {
+                finish_tile(key, off, std::true_type{}, std::true_type{});
+                key += KT;
+                off = after(off);
+            }
+            finish_tile(key, off, std::false_type{}, std::true_type{});
+        } else {
+            // (one key block: a tile begins and ends by itself)
+            while (true) {
+                finish_tile(key, off, std::false_type{}, std::true_type{});
+                if (key + KT >= see_last) break;
+                key += KT;
+                off = after(off);
+                begin_tile(key, off);
+            }
         }
+        key += KT;
+        off = after(off);
+    }
+    // tiles of which no row of the wave sees any
+    for (; key < key1; key += KT, off = after(off)) {
+        meet(key, off);
+        stage_ahead(key, off);
     }
 
-    // ---- results: register i of block m is channel 32 m + (i & 3) + 8 (i >> 2) + 4 half
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const float total = sum_halves(sum[g]);
+    // ---- results of the 32 rows from row x of the block on; register i of block m is
+    // channel 32 m + (i & 3) + 8 (i >> 2) + 4 half.  `own`: 8 KiB of LDS for the wave.
+    auto put_rows = [&](int x, f32x16 (&o)[4], float ref, float sum, uint8_t* own) __attribute__((always_inline)) {
+        const float total = sum_halves(sum);
         // weights that all vanish leave 0 here; whether that is a row without keys is
         // decided below, by what the row sees
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-        const int r = r0 + 32 * g + col;
+        const int r = x + col;
         if (part >= 0) {
-            if (r >= q_rows) continue;
+            if (r >= q_rows) return;
             const int64_t row = (static_cast<int64_t>(part) * a.H + head) * S::rows + r;
-            float* o = a.part_o + row * kValue + 4 * half;
+            float* to = a.part_o + row * kValue + 4 * half;
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<float4*>(o + 32 * m + 2 * i) =
-                        make_float4(acc[g][m][i] * inv, acc[g][m][i + 1] * inv, acc[g][m][i + 2] * inv, acc[g][m][i + 3] * inv);
+                    *reinterpret_cast<float4*>(to + 32 * m + 2 * i) = make_float4(o[m][i] * inv, o[m][i + 1] * inv, o[m][i + 2] * inv, o[m][i + 3] * inv);
             if (half == 0) {
-                a.part_m[row] = ref[g];
+                a.part_m[row] = ref;
                 a.part_l[row] = total;
             }
-            continue;
+            return;
         }
         // a row that sees no key is 0 (lse -inf); one whose keys all weigh nothing is not a number
         const bool none = sees(r) <= key0;
         const float scale = none || total != 0.0f ? inv : NAN;
         if (a.lse != nullptr && half == 0 && r < q_rows)
-            a.lse[(static_cast<int64_t>(q_row) + r) * a.H + head] = none ? -INFINITY : (ref[g] + log2f(total)) * 0.6931471805599453f;
+            a.lse[(static_cast<int64_t>(q_row) + r) * a.H + head] = none ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
         // Through LDS, so that a store instruction writes whole rows: 32 rows of 256
-        // bytes, 16 bytes c of row x at place c ^ (x & 15).  The wave's own place in the
-        // two buffers that hold no tile any more.
-        uint8_t* const own = smem + (off + (wave * G + g) * 32 * 256) % (S::buffers * S::tile);
+        // bytes, 16 bytes c of row y at place c ^ (y & 15).
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const int c = 4 * m + (i >> 2);
                 *reinterpret_cast<uint2*>(own + col * 256 + ((c ^ (col & 15)) << 4) + 8 * half) =
-                    make_uint2(kc::pack_bf16x2(acc[g][m][i] * scale, acc[g][m][i + 1] * scale),
-                               kc::pack_bf16x2(acc[g][m][i + 2] * scale, acc[g][m][i + 3] * scale));
+                    make_uint2(kc::pack_bf16x2(o[m][i] * scale, o[m][i + 1] * scale), kc::pack_bf16x2(o[m][i + 2] * scale, o[m][i + 3] * scale));
             }
         // (a wave reads back only what it wrote: LDS accesses of a wave are in order)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int x = 4 * i + (lane >> 4), c = lane & 15;
-            const uint4 y = *reinterpret_cast<const uint4*>(own + x * 256 + ((c ^ (x & 15)) << 4));
-            if (r0 + 32 * g + x < q_rows)
-                *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(q_row) + r0 + 32 * g + x) * a.out_stride_t +
-                                          static_cast<int64_t>(head) * a.out_stride_h + 8 * c) = y;
+            const int y = 4 * i + (lane >> 4), c = lane & 15;
+            const uint4 z = *reinterpret_cast<const uint4*>(own + y * 256 + ((c ^ (y & 15)) << 4));
+            if (x + y < q_rows)
+                *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(q_row) + x + y) * a.out_stride_t +
+                                          static_cast<int64_t>(head) * a.out_stride_h + 8 * c) = z;
         }
+    };
+
+    // Whether any wave wants the rows done over (a finite sum below kMost, of weights
+    // >= 0, had no block at or over it).
+#pragma unroll
+    for (int g = 0; g < G; ++g) careful = careful || __ballot(!(sum[g] < kMost)) != 0;
+    if (lane == 0) flags[S::buffers * NW + wave] = careful;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) any |= flags[S::buffers * NW + i];
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) == 0, 1)) {
+        // in the place of the tiles, which no wave reads any more
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            put_rows(r0 + 32 * g, acc[g], ref[g], sum[g], smem + (wave * G + g) * 32 * 256);
+        }
+        return;
+    }
+
+    // careful_rows: 32 rows of a wave at a time, a tile at a time.
+#pragma unroll 1
+    for (int g = 0; g < G; ++g) {
+        const int x = r0 + 32 * g;
+        const int limit = sees(x + col);
+        const int64_t qr = q_row + min(x + col, q_rows - 1);
+        const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(head) * a.q_nope.stride_h + 8 * half;
+        const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(head) * a.q_rope.stride_h + 8 * half;
+        bf16x8 qc[12];
+#pragma unroll
+        for (int ks = 0; ks < 12; ++ks) qc[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
+        f32x16 o[4] = {};
+        float rc = kUnset, sc = 0.0f;
+#pragma unroll 1
+        for (int kc0 = key0; kc0 < key1; kc0 += KT) {
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");       // no wave reads the tile before
+            stage(kc0, 0);
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
+            uint32_t found = 0;
+#pragma unroll 1
+            for (int i = lane * 16; i < 2 * S::plane; i += 1024) {
+                const uint4 y = *reinterpret_cast<const uint4*>(smem + S::value_at + i);
+                const uint32_t w4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+            }
+            const bool odd = __ballot(found != 0) != 0;
+#pragma unroll 1
+            for (int b = 0; b < KB; ++b) {
+                f32x16 z = {};
+#pragma unroll
+                for (int ks = 0; ks < 12; ++ks)
+                    z = mfma(*reinterpret_cast<const bf16x8*>(smem + ka[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow), qc[ks], z);
+                const int seen_here = limit - kc0 - 32 * b - 4 * half;
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    z[i] = (i & 3) + 8 * (i >> 2) < seen_here ? z[i] : -INFINITY;
+                    top = fmaxf(top, z[i]);
+                }
+                const float to = fminf(fmaxf(rc, max_halves(top) * c2), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
+                const float f = __builtin_amdgcn_exp2f(rc - to);
+                rc = to;
+                sc *= f;
+                uint32_t pairs[8];
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(z[i], c2, -rc)), e1 = __builtin_amdgcn_exp2f(fmaf(z[i + 1], c2, -rc));
+                    sc += e0;
+                    sc += e1;
+                    pairs[i >> 1] = kc::pack_bf16x2(e0, e1);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[m][i] *= f;
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) {
+                        const uint8_t* at = smem + va[m & 1] + (m >> 1) * S::plane + (2 * b + ks) * 16 * kRow;
+                        const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
+                        const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kRow));
+                        i16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+                        // values that are not finite are left out of the product ...
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = (v[j] & 0x7F80) == 0x7F80 ? 0 : v[j];
+                        const u32x4 p4 = {pairs[4 * ks], pairs[4 * ks + 1], pairs[4 * ks + 2], pairs[4 * ks + 3]};
+                        o[m] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p4), o[m]);
+                    }
+                }
+            }
+            // ... and added to the rows that see them, to which they give what they are
+            if (odd) {
+#pragma unroll 1
+                for (int j = 0; j < KT; ++j) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
+                            const uint32_t bits = *reinterpret_cast<const uint16_t*>(
+                                smem + S::value_at + (m >> 1) * S::plane + j * kRow + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
+                            o[m][i] += (bits & 0x7F80u) == 0x7F80u && kc0 + j < limit ? __uint_as_float(bits << 16) : 0.0f;
+                        }
+                }
+            }
+        }
+        put_rows(x, o, rc, sc, smem + S::tile + wave * 32 * 256);
     }
 }
 
