@@ -126,7 +126,7 @@ struct Lengths {
     int32_t B, causal;
 };
 
-// Calls f(q_row, rows, kv_row, key1, seen0, kv_len) for every block of `rows` query rows.
+// Calls f(b, q_row, rows, kv_row, key1, seen0) for every block of `rows` query rows.
 template <typename F>
 void each_block(const Lengths& n, int32_t rows, F f) {
     int64_t q_at = 0, kv_at = 0;
@@ -138,7 +138,7 @@ void each_block(const Lengths& n, int32_t rows, F f) {
             const int32_t r = std::min(rows, q - i);
             const int32_t key1 = n.causal ? std::clamp(kv - q + i + r, 0, kv) : kv;
             const int32_t seen0 = n.causal ? kv - q + i + 1 : mla::kPrefillUnmasked;
-            f(q_row + i, r, kv_row, key1, seen0, kv);
+            f(b, q_row + i, r, kv_row, key1, seen0);
         }
         q_at += q;
         kv_at += kv;
@@ -157,9 +157,13 @@ int32_t splits_of(int32_t tiles, int64_t most) {
 struct Shape {
     int32_t rows, slots, least_tiles;
 };
-constexpr Shape kShapes[] = {{32, 512, 4}, {128, 256, 8}, {256, 256, 8}};
+constexpr Shape kShapes[] = {{32, 512, 4}, {128, 512, 8}, {256, 256, 8}};
+
+thread_local int32_t g_rows = 0;       // mla_internal_prefill_rows
 
 Shape choose_rows(const Lengths& n) {
+    for (const Shape& s : kShapes)
+        if (s.rows == g_rows) return s;
     int32_t most = 0;
     for (int32_t b = 0; b < n.B; ++b) most = std::max(most, n.q[b]);
     return most <= 32 ? kShapes[0] : most <= 128 ? kShapes[1] : kShapes[2];
@@ -196,6 +200,76 @@ int check_lengths(const Lengths& n, int64_t* total_q, int64_t* total_kv) {
     return st;
 }
 
+int64_t plan_ints(const mla_prefill_plan& p) {
+    const mla::PrefillLists l = mla::prefill_lists(p.num_items, p.H, p.rows);
+    return (static_cast<int64_t>(p.num_items) + p.num_merges) * mla::kPrefillRecordInts + (l.lists > 0 ? l.lists + 1 + l.entries : 0);
+}
+
+// Deals (item, head) out to the lists as workgroups would take them, each when it
+// is done with the one before: sequence by sequence, a sequence's heads one after
+// the other, so that the blocks of a head's rows run at the same time and read its
+// keys through one L2; the last rounds by length, so that the short ones fill the
+// end.  Blocks that begin together go through their keys from the first on; where
+// the lists are spread out, the longest block begins first and all end together,
+// so they go from the last key down: either way they read the same keys at the
+// same time.  `items` in the order of the plan.
+constexpr int32_t kItemTiles = 5;       // an item's fixed cost, in tiles
+constexpr int32_t kLastRounds = 2;
+constexpr int32_t kL2Tiles = 96;        // tiles of a head that fill an XCD's L2 (40 KiB each)
+void fill_lists(const mla::PrefillItem* items, const mla_prefill_plan& p, int32_t* out) {
+    const mla::PrefillLists l = mla::prefill_lists(p.num_items, p.H, p.rows);
+    const auto tiles = [&](int32_t i) { return tiles_of(items[i].key1 - items[i].key0); };
+    struct Load {
+        int64_t tiles;
+        int32_t list;
+    };
+    constexpr int32_t kMostLists = 256;
+    Load heap[kMostLists];
+    int32_t filled[kMostLists], last[kLastRounds * kMostLists];
+    const auto later = [](const Load& x, const Load& y) { return x.tiles != y.tiles ? x.tiles > y.tiles : x.list > y.list; };
+    const int64_t sorted_from = std::max<int64_t>(0, l.entries - kLastRounds * l.lists);
+    // gives f(list, entry) for all entries
+    const auto deal = [&](auto f) {
+        for (int32_t i = 0; i < l.lists; ++i) heap[i] = {0, i};         // (equal: a heap)
+        const auto give = [&](int32_t entry, bool down) {
+            std::pop_heap(heap, heap + l.lists, later);
+            Load& to = heap[l.lists - 1];
+            f(to.list, down ? ~entry : entry);
+            to.tiles += kItemTiles + tiles(entry / l.heads);
+            std::push_heap(heap, heap + l.lists, later);
+        };
+        int64_t at = 0;
+        int32_t n = 0;
+        for (int32_t from = 0, to; from < p.num_items; from = to) {
+            for (to = from + 1; to < p.num_items && items[to].seq == items[from].seq;) ++to;
+            for (int32_t h = 0; h < l.heads; ++h)
+                for (int32_t i = from; i < to;) {
+                    const int32_t round_end = std::min(i + l.lists, to);
+                    const Load& latest = *std::min_element(heap, heap + l.lists, later);
+                    const bool down = tiles(i) >= kL2Tiles && 2 * (latest.tiles - heap[0].tiles) > tiles(i) - tiles(round_end - 1);
+                    for (; i < round_end; ++i, ++at) {
+                        if (at < sorted_from) give(i * l.heads + h, down);
+                        else last[n++] = i * l.heads + h;
+                    }
+                }
+        }
+        std::sort(last, last + n, [&](int32_t x, int32_t y) {
+            const int32_t tx = tiles(x / l.heads), ty = tiles(y / l.heads);
+            return tx != ty ? tx > ty : x < y;
+        });
+        for (int32_t i = 0; i < n; ++i) give(last[i], false);
+    };
+    int32_t* const first = out;
+    int32_t* const entries = out + l.lists + 1;
+    std::fill(first, first + l.lists + 1, 0);
+    deal([&](int32_t list, int32_t) { ++first[list + 1]; });
+    for (int32_t i = 0; i < l.lists; ++i) {
+        first[i + 1] += first[i];
+        filled[i] = first[i];
+    }
+    deal([&](int32_t list, int32_t entry) { entries[filled[list]++] = entry; });
+}
+
 int check_head_rows(const mla_head_rows* r, bool heads, mla::HeadRows* out) {
     if (r == nullptr || r->data == nullptr) return MLA_EINVAL;
     const int64_t h = heads ? r->stride_h : 0;
@@ -215,6 +289,10 @@ bool rows_apart(int64_t stride_t, int64_t stride_h, int64_t T, int64_t H, int64_
 }
 
 }  // namespace
+
+namespace mla {
+extern "C" void mla_internal_prefill_rows(int32_t rows) { g_rows = rows; }
+}  // namespace mla
 
 extern "C" {
 
@@ -349,12 +427,12 @@ int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_
     // where whole blocks would leave slots empty or one slot far behind.
     const Shape shape = choose_rows(n);
     int64_t tiles = 0;
-    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t, int32_t key1, int32_t, int32_t) { tiles += tiles_of(key1); });
+    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t, int32_t, int32_t key1, int32_t) { tiles += tiles_of(key1); });
     // (tiles <= 2^30 blocks x 2^24 tiles, and H < 2^31: in double, its rounding is of no matter here)
     const int64_t most = std::max<int64_t>(
         shape.least_tiles, static_cast<int64_t>(std::ceil(static_cast<double>(tiles) * H / shape.slots)));
     int64_t items = 0, merges = 0, parts = 0;
-    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t, int32_t key1, int32_t, int32_t) {
+    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t, int32_t, int32_t key1, int32_t) {
         const int32_t s = splits_of(tiles_of(key1), most);
         items += s;
         if (s > 1) {
@@ -373,7 +451,7 @@ int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_
     p.num_items = static_cast<int32_t>(items);
     p.num_merges = static_cast<int32_t>(merges);
     p.num_parts = static_cast<int32_t>(parts);
-    p.plan_ints = (items + merges) * mla::kPrefillRecordInts;
+    p.plan_ints = plan_ints(p);
     p.workspace_bytes = parts * H * shape.rows * mla::kPartRowBytes;
     *info = p;
     if (plan == nullptr) return MLA_OK;
@@ -383,23 +461,36 @@ int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_
     auto* merge = reinterpret_cast<mla::PrefillMerge*>(item + items);
     mla::PrefillItem* const first_item = item;
     int32_t part = 0;
-    each_block(n, shape.rows, [&](int32_t q_row, int32_t rows, int32_t kv_row, int32_t key1, int32_t seen0,
-                                  int32_t kv_len) {
+    each_block(n, shape.rows, [&](int32_t b, int32_t q_row, int32_t rows, int32_t kv_row, int32_t key1, int32_t seen0) {
         const int32_t t = tiles_of(key1), s = splits_of(t, most);
         const int32_t per = (t + s - 1) / s * kKeyTile;
-        if (s > 1) *merge++ = {q_row, rows, part, s, seen0, kv_len, {0, 0}};
+        if (s > 1) *merge++ = {q_row, rows, part, s, seen0, kv_lens[b], {0, 0}};
         for (int32_t k = 0; k < s; ++k) {
             const int64_t from = static_cast<int64_t>(k) * per;
             *item++ = {q_row, rows, kv_row, static_cast<int32_t>(std::min<int64_t>(from, key1)),
-                       static_cast<int32_t>(std::min<int64_t>(from + per, key1)), seen0, s > 1 ? part++ : -1, 0};
+                       static_cast<int32_t>(std::min<int64_t>(from + per, key1)), seen0, s > 1 ? part++ : -1, b};
         }
     });
-    // the longest first, so that the short ones fill the launch's end
-    std::sort(first_item, item, [](const mla::PrefillItem& x, const mla::PrefillItem& y) {
-        const int32_t a = tiles_of(x.key1 - x.key0), b = tiles_of(y.key1 - y.key0);
-        if (a != b) return a > b;
+    const auto len = [](const mla::PrefillItem& x) { return tiles_of(x.key1 - x.key0); };
+    const auto in_order = [](const mla::PrefillItem& x, const mla::PrefillItem& y) {
         return x.q_row != y.q_row ? x.q_row < y.q_row : x.key0 < y.key0;
+    };
+    if (shape.rows != mla::kListedRows) {
+        // the longest first, so that the short ones fill the launch's end
+        std::sort(first_item, item, [&](const mla::PrefillItem& x, const mla::PrefillItem& y) {
+            return len(x) != len(y) ? len(x) > len(y) : in_order(x, y);
+        });
+        return MLA_OK;
+    }
+    // sequence by sequence, the longest first, and so within a sequence
+    std::sort(first_item, item, [&](const mla::PrefillItem& x, const mla::PrefillItem& y) {
+        if (x.seq != y.seq) {
+            const int32_t kx = kv_lens[x.seq], ky = kv_lens[y.seq];
+            return kx != ky ? kx > ky : x.seq < y.seq;
+        }
+        return len(x) != len(y) ? len(x) > len(y) : in_order(x, y);
     });
+    fill_lists(first_item, p, plan + (items + merges) * mla::kPrefillRecordInts);
     return MLA_OK;
 }
 
@@ -414,8 +505,7 @@ int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan, const ml
     if (info->num_items < 0 || info->num_merges < 0 || info->num_parts < 0 || info->total_q < 0 ||
         info->total_kv < 0 || info->total_q > kMaxLen || info->total_kv > kMaxLen)
         return MLA_EINVAL;
-    if (info->plan_ints != (static_cast<int64_t>(info->num_items) + info->num_merges) * mla::kPrefillRecordInts)
-        return MLA_EINVAL;
+    if (info->plan_ints != plan_ints(*info)) return MLA_EINVAL;
     if (info->num_items == 0) return MLA_OK;
     bool known = false;
     for (const Shape& s : kShapes) known = known || s.rows == info->rows;
@@ -449,6 +539,7 @@ int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan, const ml
     }
     a.items = reinterpret_cast<const mla::PrefillItem*>(plan);
     a.merges = reinterpret_cast<const mla::PrefillMerge*>(a.items + info->num_items);
+    if (info->rows == mla::kListedRows) a.first = reinterpret_cast<const int32_t*>(a.merges + info->num_merges);
     a.num_items = info->num_items;
     a.num_merges = info->num_merges;
     a.num_parts = info->num_parts;

@@ -64,7 +64,7 @@ using kc::lds_i16x4;
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kMost = 0x1p100f;
+constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;
 constexpr float kUnset = -FLT_MAX;
 
 // Score products accumulate in vector registers, with the queries in accumulation
@@ -117,12 +117,13 @@ struct Shape {
     static constexpr int loads = 5 * blocks / NW;           // per wave
     static_assert(blocks % NW == 0, "a wave's load belongs to one plane");
     static constexpr int buffers = 3;
+    static constexpr bool listed = rows == kListedRows;     // goes through a list of blocks
     static constexpr int lds = buffers * tile + (buffers + 1) * NW * 4;
-    static_assert(lds <= 160 * 1024 && NW * G * kRowsPerWave * 256 <= (buffers - 1) * tile, "LDS; results beside the last tile");
+    static_assert(lds <= 160 * 1024 && NW * kRowsPerWave * 256 <= (listed ? 1 : buffers - 1) * tile, "LDS; results in the place of tiles");
 };
 
 template <int NW, int G, int KT>
-__global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
+__global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(PrefillArgs a) {
     using S = Shape<NW, G, KT>;
     constexpr int KB = S::kb;
     __shared__ __align__(1024) uint8_t smem[S::buffers * S::tile];
@@ -132,55 +133,82 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const int half = lane >> 5, col = lane & 31;
 
-    // Workgroup -> (head, item).  Workgroup i runs on XCD i mod 8: where the heads
-    // divide by 8 an XCD takes whole heads, one after the other, so that the
-    // blocks of a head's rows read its keys through one L2.
+    // Workgroup -> (item, head).  Workgroup i runs on XCD i mod 8: where the heads
+    // divide by 8 an XCD takes whole heads, so that the blocks of a head's rows read
+    // its keys through one L2.
+    struct Block {
+        int head, q_row, q_rows, kv_row, key0, key1, seen0, part;
+        int tiles;
+        bool down;          // the tiles from the last to the first
+    };
     const int wg = static_cast<int>(blockIdx.x);
-    int head, item_id;
-    if ((a.H & 7) == 0) {
-        const int k = wg >> 3;
-        const int h = k / a.num_items;
-        head = (wg & 7) * (a.H >> 3) + h;
-        item_id = k - h * a.num_items;
-    } else {
-        item_id = wg / a.H;
-        head = wg - item_id * a.H;
+    const bool by_xcd = (a.H & 7) == 0;
+    const int heads = by_xcd ? a.H >> 3 : a.H, head0 = by_xcd ? (wg & 7) * heads : 0;
+    const int list = by_xcd ? wg >> 3 : wg;
+    auto block_of = [&](int entry) __attribute__((always_inline)) {
+        // indices from the plan, kept inside the tensors whatever it holds
+        const bool down = S::listed && entry < 0;
+        const uint32_t e = static_cast<uint32_t>(down ? ~entry : entry), item = e / static_cast<uint32_t>(heads);
+        const PrefillItem* const ip = a.items + min(item, static_cast<uint32_t>(a.num_items - 1));
+        Block x;
+        x.head = head0 + static_cast<int>(e - item * static_cast<uint32_t>(heads));
+        x.q_row = min(max(ip->q_row, 0), a.total_q - 1);
+        x.q_rows = min(min(max(ip->q_rows, 1), S::rows), a.total_q - x.q_row);
+        x.kv_row = min(max(ip->kv_row, 0), a.total_kv);
+        x.key1 = min(max(ip->key1, 0), a.total_kv - x.kv_row);
+        x.key0 = min(max(ip->key0, 0), x.key1);
+        x.seen0 = ip->seen0;
+        x.part = min(ip->part, a.num_parts - 1);
+        x.tiles = (x.key1 - x.key0 + KT - 1) / KT;
+        x.down = down;
+        return x;
+    };
+    // a list's entries, for a workgroup of 256 rows (the launch has one per list)
+    int at = 0, end = 1;
+    const int32_t* entries = nullptr;
+    if constexpr (S::listed) {
+        const int lists = by_xcd ? static_cast<int>(gridDim.x >> 3) : static_cast<int>(gridDim.x);
+        const int most = a.num_items * heads;
+        entries = a.first + lists + 1;
+        at = min(max(a.first[list], 0), most);
+        end = min(a.first[list + 1], most);
+        if (at >= end) return;
     }
-    const PrefillItem* ip = a.items + item_id;
-    // indices from the plan, kept inside the tensors whatever it holds
-    const int q_row = min(max(ip->q_row, 0), a.total_q - 1);
-    const int q_rows = min(min(max(ip->q_rows, 1), S::rows), a.total_q - q_row);
-    const int kv_row = min(max(ip->kv_row, 0), a.total_kv);
-    const int key1 = min(max(ip->key1, 0), a.total_kv - kv_row);
-    const int key0 = min(max(ip->key0, 0), key1);
-    const int seen0 = ip->seen0;
-    const int part = min(ip->part, a.num_parts - 1);
+    Block cur = block_of(S::listed ? entries[at] : list);
 
-    // keys that row x of the block sees
-    auto sees = [&](int x) { return static_cast<int>(min(static_cast<int64_t>(key1), static_cast<int64_t>(seen0) + x)); };
-    const int r0 = wave * G * kRowsPerWave;         // the wave's first row of the block
-    const int see_block = sees(0), see_first = sees(r0);
-    const int r_last = min(r0 + G * kRowsPerWave, q_rows) - 1;
-    const int see_last = r_last < r0 ? key0 : sees(r_last);     // the most keys that a row of this wave sees
+    const int r0 = wave * G * kRowsPerWave;         // the wave's first row of a block
+    // a block's tile t, in the order in which they are gone through
+    auto key_of = [&](const Block& b, int t) __attribute__((always_inline)) { return b.key0 + KT * (b.down ? b.tiles - 1 - t : t); };
+    // keys that row x of a block sees
+    auto sees_of = [&](const Block& b, int x) { return static_cast<int>(min(static_cast<int64_t>(b.key1), static_cast<int64_t>(b.seen0) + x)); };
 
     // ---- staging ----------------------------------------------------------
     const uint32_t kn_b = static_cast<uint32_t>(a.k_nope.stride_t * 2), kr_b = static_cast<uint32_t>(a.k_rope.stride_t * 2),
                    vv_b = static_cast<uint32_t>(a.v.stride_t * 2);
-    const uint8_t* const kn = reinterpret_cast<const uint8_t*>(a.k_nope.data + static_cast<int64_t>(head) * a.k_nope.stride_h) +
-                              static_cast<int64_t>(kv_row) * kn_b;
-    const uint8_t* const kr = reinterpret_cast<const uint8_t*>(a.k_rope.data) + static_cast<int64_t>(kv_row) * kr_b;
-    const uint8_t* const vv = reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(head) * a.v.stride_h) +
-                              static_cast<int64_t>(kv_row) * vv_b;
+    // rows of key `key` of a block
+    auto nope_at = [&](const Block& b, int key) __attribute__((always_inline)) {
+        return reinterpret_cast<const uint8_t*>(a.k_nope.data + static_cast<int64_t>(b.head) * a.k_nope.stride_h) + (static_cast<int64_t>(b.kv_row) + key) * kn_b;
+    };
+    auto rope_at = [&](const Block& b, int key) __attribute__((always_inline)) {
+        return reinterpret_cast<const uint8_t*>(a.k_rope.data) + (static_cast<int64_t>(b.kv_row) + key) * kr_b;
+    };
+    auto value_at = [&](const Block& b, int key) __attribute__((always_inline)) {
+        return reinterpret_cast<const uint8_t*>(a.v.data + static_cast<int64_t>(b.head) * a.v.stride_h) + (static_cast<int64_t>(b.kv_row) + key) * vv_b;
+    };
     const uint32_t lds0 = kc::lds_addr(smem);
+    // The lane, for what is used once per block: what follows from it is not worth
+    // registers across the loops.
+    auto fresh_lane = [&]() __attribute__((always_inline)) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
     // A wave's loads of a tile: i * NW + wave counts the tile's 8-row blocks, plane by
     // plane.  Rows past the range's end re-read its last key.
-    auto stage = [&](int key, int to) __attribute__((always_inline)) {
-        const int last = key1 - 1 - key;
-        int l = lane;
-        asm volatile("" : "+v"(l));         // (what follows from it is not worth registers across the loops)
-        const uint8_t* const n = kn + static_cast<int64_t>(key) * kn_b;
-        const uint8_t* const r = kr + static_cast<int64_t>(key) * kr_b;
-        const uint8_t* const v = vv + static_cast<int64_t>(key) * vv_b;
+    auto stage = [&](const Block& b, int key, int to) __attribute__((always_inline)) {
+        const int last = b.key1 - 1 - key;
+        const int l = fresh_lane();
+        const uint8_t *const n = nope_at(b, key), *const r = rope_at(b, key), *const v = value_at(b, key);
 #pragma unroll
         for (int i = 0; i < S::loads; ++i) {
             const int plane = i * NW / S::blocks, block = i * NW % S::blocks + wave;
@@ -212,7 +240,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     // there, of the tiles that some row sees in part; `flags` says whether any wave
     // found one that is not finite (the buffer's NW words).
     auto look = [&](int key, int to) __attribute__((always_inline)) {
-        if (key + KT <= see_block) return;
+        if (key + KT <= sees_of(cur, 0)) return;
         uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < S::loads; ++i) {
@@ -236,34 +264,59 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     auto after = [&](int off) __attribute__((always_inline)) { return off == (S::buffers - 1) * S::tile ? 0 : off + S::tile; };
     // Once per tile, anywhere in a wave's work on it: the next tile is there, and no
     // wave reads the one before any more.
-    auto meet = [&](int key, int off) __attribute__((always_inline)) {
+    auto meet = [&](int t, int off) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        if (key + KT < key1) look(key + KT, after(off));
+        if (t + 1 < cur.tiles) look(key_of(cur, t + 1), after(off));
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
     };
-    auto stage_ahead = [&](int key, int off) __attribute__((always_inline)) {
-        if (key + 2 * KT < key1) stage(key + 2 * KT, after(after(off)));
+    // The tile after the next, past the block's end one of the first two of the next
+    // block (of `following`, if there is one).
+    Block following = cur;
+    bool more = false;
+    auto stage_ahead = [&](int t, int off) __attribute__((always_inline)) {
+        const int left = cur.tiles - t;
+        if (left > 2) return stage(cur, key_of(cur, t + 2), after(after(off)));
+        if constexpr (S::listed) {
+            if (!more) return;
+            if (following.tiles > 0 && (left == 2 || t == 0))
+                stage(following, key_of(following, 0), left == 2 ? after(after(off)) : after(off));
+            if (following.tiles > 1 && left == 1) stage(following, key_of(following, 1), after(after(off)));
+        }
     };
-    if (key0 < key1) stage(key0, 0);
 
     // ---- queries: operand B of step ks holds channels 16 ks + 8 half .. + 7 of the
     // lane's row of the group
     bf16x8 q[G][12];
+    auto load_queries = [&](const Block& b) __attribute__((always_inline)) {
+        const int l = fresh_lane(), col = l & 31, half = l >> 5;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const int64_t qr = q_row + min(r0 + 32 * g + col, q_rows - 1);
-        const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(head) * a.q_nope.stride_h + 8 * half;
-        const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(head) * a.q_rope.stride_h + 8 * half;
+        for (int g = 0; g < G; ++g) {
+            const int64_t qr = b.q_row + min(r0 + 32 * g + col, b.q_rows - 1);
+            const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(b.head) * a.q_nope.stride_h + 8 * half;
+            const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(b.head) * a.q_rope.stride_h + 8 * half;
 #pragma unroll
-        for (int ks = 0; ks < 12; ++ks)
-            q[g][ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
-    }
-    // (waited for here: the wait that the compiler would put into the loop, for
-    // its first pass, would hold every pass up until the next tile is staged)
+            for (int ks = 0; ks < 12; ++ks)
+                q[g][ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
+        }
+    };
+    // A block's first two tiles, where no block before it had tiles to stage them from.
+    auto stage_first = [&](const Block& b, int off) __attribute__((always_inline)) {
+        if (b.tiles > 0) stage(b, key_of(b, 0), off);
+        if (b.tiles > 1) stage(b, key_of(b, 1), after(off));
+    };
+    // (waited for here: the wait that the compiler would put into the loop over the
+    // tiles, for its first pass, would hold every pass up until the next tile is staged)
+    auto settle = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int ks = 0; ks < 12; ++ks) asm volatile("" : "+a"(q[g][ks]));
+            for (int ks = 0; ks < 12; ++ks) asm volatile("" : "+a"(q[g][ks]));
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    };
+    int off = 0;
+    stage_first(cur, off);
+    load_queries(cur);
+    settle();
 
     // ---- LDS read addresses of the lane; planes, blocks and steps are immediate
     // offsets
@@ -298,28 +351,14 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
 
     f32x16 acc[G][4];
     float ref[G], sum[G];                   // reference, sum of the weights
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        ref[g] = kUnset;
-        sum[g] = 0.0f;
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[g][m][i] = 0.0f;
-    }
     const float c2 = a.scale_log2;
-    bool careful = false;                   // whether the rows have to be done over
+    bool careful;                           // whether the rows have to be done over
+    int see_block;                          // keys that the block's first row sees
 
     // register i of block b is key `key + 32 b + (i & 3) + 8 (i >> 2) + 4 half`
     f32x16 s[KB][G];
     uint32_t w[G][8 * KB];                  // weights, bf16 pairs
     float block_sum[G];
-    auto hide = [&](int b, int g, int key) __attribute__((always_inline)) {
-        const int here = sees(r0 + 32 * g + col) - key - 4 * half;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (32 * b + (i & 3) + 8 * (i >> 2) >= here) s[b][g][i] = -INFINITY;
-    };
     // the row's largest score of block b, log2 units
     auto top_of = [&](int b, int g) __attribute__((always_inline)) {
         float top = s[b][g][0];
@@ -398,7 +437,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
     int here[G];                                // keys of the tile that the lane's rows see, less 4 half
     auto set_here = [&](int key) __attribute__((always_inline)) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) here[g] = sees(r0 + 32 * g + col) - key - 4 * half;
+        for (int g = 0; g < G; ++g) here[g] = sees_of(cur, r0 + 32 * g + col) - key - 4 * half;
     };
     auto unit = [&](int b, int u, bool hide) __attribute__((always_inline)) {
         if (u >= 2 && u - 2 < kWeights) {
@@ -442,40 +481,40 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         take_sums();
     };
     const uint8_t *next_n, *next_r, *next_v;    // rows of the tile after the next
-    // A of a tile by itself, and its early weights; the first tile of all sets the
+    int64_t step_n, step_r, step_v;             // from a tile's rows to the next tile's
+    // A of a tile by itself, and its early weights; the wave's first tile sets the
     // references.  Ends with B's (or C's) operands on their way.
-    auto begin_tile = [&](int key, int off) __attribute__((always_inline)) {
+    auto begin_tile = [&](int t, int off, bool first) __attribute__((always_inline)) {
         set_tile(off);
-        set_here(key);
+        set_here(key_of(cur, t));
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) ring[j] = key_operand(kt, j);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (KB == 2) score_phase(0, keys_of(1), nothing);
         else score_phase(0, values_of(0), nothing);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            scores_ready(s[0][g]);
-            if (key + KT > see_first) hide(0, g, key);
-        }
-        if (key == key0) {
+        for (int g = 0; g < G; ++g) scores_ready(s[0][g]);
+        if (first) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, top_of(0, g));      // (no key: any finite value)
+            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, top_of(0, g));
         }
 #pragma unroll
-        for (int u = 0; u < kEarly; ++u) unit(0, u, false);
+        for (int u = 0; u < kEarly; ++u) unit(0, u, true);
     };
-    // The rest of a tile after begin_tile; kNext: with the next tile's A and early
+    // The rest of tile t after begin_tile; kNext: with the next tile's A and early
     // weights, else by itself.  kPart: some row of the wave may not see all of it (or of
     // the next); otherwise it and the next are whole, and another whole one is behind
     // them.  `careful` is set where the tile is not for this path.
-    auto finish_tile = [&](int key, int off, auto with_next, auto in_part) __attribute__((always_inline)) {
+    auto finish_tile = [&](int t, int off, auto with_next, auto in_part) __attribute__((always_inline)) {
         constexpr bool kNext = decltype(with_next)::value, kPart = decltype(in_part)::value;
         const int next = after(off);
         const uint32_t to = after(next);
-        meet(key, off);
+        meet(t, off);
         if constexpr (kPart) {
-            stage_ahead(key, off);
+            stage_ahead(t, off);
+            const int key = key_of(cur, t);
             careful = careful || (key + KT > see_block && odd_values(off));
+            set_here(key);
         }
         // (spread over the 20 G slots of B and C)
         auto load_slot = [&](int slot) __attribute__((always_inline)) {
@@ -504,19 +543,20 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
                 score_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { late(1, slot, kPart); });
                 if constexpr (kPart) {
 #pragma unroll
-                    for (int g = 0; g < G; ++g) here[g] -= KT;
+                    for (int g = 0; g < G; ++g) here[g] += cur.down ? KT : -KT;
                 }
                 value_phase(1, keys_of(1), [&](int slot) __attribute__((always_inline)) {
                     early(0, slot, kPart);
                     if (!kPart && slot == 0) {
-                        next_n += static_cast<uint64_t>(KT) * kn_b;
-                        next_r += static_cast<uint64_t>(KT) * kr_b;
-                        next_v += static_cast<uint64_t>(KT) * vv_b;
+                        next_n += step_n;
+                        next_r += step_r;
+                        next_v += step_v;
                     }
                 });
 #pragma unroll
                 for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], next);
             } else {
+                if (more) load_queries(following);      // (no score product of this block is left)
                 value_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { early(1, slot, kPart); });
                 weigh_rest(1, kEarly, kPart);
                 value_phase(1, keep, nothing);
@@ -524,66 +564,18 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
         }
     };
 
-    if (key0 < key1) {
-        if (key0 + KT < key1) {
-            stage(key0 + KT, S::tile);
-            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(S::loads) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        }
-        look(key0, 0);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    }
-    int key = key0, off = 0;
-    if (key < see_last) {
-        begin_tile(key, off);
-        if constexpr (KB == 2) {
-            const int last_followed = min(see_first - 2 * KT, key1 - 3 * KT);
-            next_n = kn + static_cast<int64_t>(key + 2 * KT) * kn_b;
-            next_r = kr + static_cast<int64_t>(key + 2 * KT) * kr_b;
-            next_v = vv + static_cast<int64_t>(key + 2 * KT) * vv_b;
-            while (key <= last_followed) {
-                finish_tile(key, off, std::true_type{}, std::false_type{});
-                key += KT;
-                off = after(off);
-            }
-            set_here(key);
-            while (key + KT < see_last) {
-                finish_tile(key, off, std::true_type{}, std::true_type{});
-                key += KT;
-                off = after(off);
-            }
-            finish_tile(key, off, std::false_type{}, std::true_type{});
-        } else {
-            // (one key block: a tile begins and ends by itself)
-            while (true) {
-                finish_tile(key, off, std::false_type{}, std::true_type{});
-                if (key + KT >= see_last) break;
-                key += KT;
-                off = after(off);
-                begin_tile(key, off);
-            }
-        }
-        key += KT;
-        off = after(off);
-    }
-    // tiles of which no row of the wave sees any
-    for (; key < key1; key += KT, off = after(off)) {
-        meet(key, off);
-        stage_ahead(key, off);
-    }
-
     // ---- results of the 32 rows from row x of the block on; register i of block m is
     // channel 32 m + (i & 3) + 8 (i >> 2) + 4 half.  `own`: 8 KiB of LDS for the wave.
     auto put_rows = [&](int x, f32x16 (&o)[4], float ref, float sum, uint8_t* own) __attribute__((always_inline)) {
+        const int l = fresh_lane(), col = l & 31, half = l >> 5;
         const float total = sum_halves(sum);
         // weights that all vanish leave 0 here; whether that is a row without keys is
         // decided below, by what the row sees
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int r = x + col;
-        if (part >= 0) {
-            if (r >= q_rows) return;
-            const int64_t row = (static_cast<int64_t>(part) * a.H + head) * S::rows + r;
+        if (cur.part >= 0) {
+            if (r >= cur.q_rows) return;
+            const int64_t row = (static_cast<int64_t>(cur.part) * a.H + cur.head) * S::rows + r;
             float* to = a.part_o + row * kValue + 4 * half;
 #pragma unroll
             for (int m = 0; m < 4; ++m)
@@ -596,11 +588,12 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
             }
             return;
         }
+        if (x >= cur.q_rows) return;
         // a row that sees no key is 0 (lse -inf); one whose keys all weigh nothing is not a number
-        const bool none = sees(r) <= key0;
+        const bool none = sees_of(cur, r) <= cur.key0;
         const float scale = none || total != 0.0f ? inv : NAN;
-        if (a.lse != nullptr && half == 0 && r < q_rows)
-            a.lse[(static_cast<int64_t>(q_row) + r) * a.H + head] = none ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+        if (a.lse != nullptr && half == 0 && r < cur.q_rows)
+            a.lse[(static_cast<int64_t>(cur.q_row) + r) * a.H + cur.head] = none ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
         // Through LDS, so that a store instruction writes whole rows: 32 rows of 256
         // bytes, 16 bytes c of row y at place c ^ (y & 15).
 #pragma unroll
@@ -611,122 +604,213 @@ __global__ __launch_bounds__(64 * NW, 1) void prefill_kernel(PrefillArgs a) {
                 *reinterpret_cast<uint2*>(own + col * 256 + ((c ^ (col & 15)) << 4) + 8 * half) =
                     make_uint2(kc::pack_bf16x2(o[m][i] * scale, o[m][i + 1] * scale), kc::pack_bf16x2(o[m][i + 2] * scale, o[m][i + 3] * scale));
             }
-        // (a wave reads back only what it wrote: LDS accesses of a wave are in order)
+        // (a wave reads back only what it wrote: LDS accesses of a wave are in order; lanes
+        // past the block's last row write that row once more)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int y = 4 * i + (lane >> 4), c = lane & 15;
+            const int y = min(4 * i + (l >> 4), cur.q_rows - 1 - x), c = l & 15;
             const uint4 z = *reinterpret_cast<const uint4*>(own + y * 256 + ((c ^ (y & 15)) << 4));
-            if (x + y < q_rows)
-                *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(q_row) + x + y) * a.out_stride_t +
-                                          static_cast<int64_t>(head) * a.out_stride_h + 8 * c) = z;
+            *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(cur.q_row) + x + y) * a.out_stride_t +
+                                      static_cast<int64_t>(cur.head) * a.out_stride_h + 8 * c) = z;
         }
     };
 
-    // Whether any wave wants the rows done over (a finite sum below kMost, of weights
-    // >= 0, had no block at or over it).
-#pragma unroll
-    for (int g = 0; g < G; ++g) careful = careful || __ballot(!(sum[g] < kMost)) != 0;
-    if (lane == 0) flags[S::buffers * NW + wave] = careful;
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) any |= flags[S::buffers * NW + i];
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) == 0, 1)) {
-        // in the place of the tiles, which no wave reads any more
+    while (true) {
+        see_block = sees_of(cur, 0);
+        // In key order: the first `whole` tiles are seen by all rows of the wave, the
+        // first `some` by any.
+        const int see_first = sees_of(cur, r0), r_last = min(r0 + G * kRowsPerWave, cur.q_rows) - 1;
+        const int whole = max(see_first - cur.key0, 0) / KT;
+        const int some = r_last < r0 ? 0 : (max(sees_of(cur, r_last) - cur.key0, 0) + KT - 1) / KT;
+        const int t_begin = cur.down ? cur.tiles - some : 0, t_end = cur.down ? cur.tiles : some;
+        if constexpr (S::listed) {
+            more = at + 1 < end;
+            if (more) following = block_of(entries[at + 1]);
+        }
+        careful = false;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            put_rows(r0 + 32 * g, acc[g], ref[g], sum[g], smem + (wave * G + g) * 32 * 256);
+            ref[g] = kUnset;
+            sum[g] = 0.0f;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[g][m][i] = 0.0f;
         }
-        return;
-    }
-
-    // careful_rows: 32 rows of a wave at a time, a tile at a time.
-#pragma unroll 1
-    for (int g = 0; g < G; ++g) {
-        const int x = r0 + 32 * g;
-        const int limit = sees(x + col);
-        const int64_t qr = q_row + min(x + col, q_rows - 1);
-        const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(head) * a.q_nope.stride_h + 8 * half;
-        const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(head) * a.q_rope.stride_h + 8 * half;
-        bf16x8 qc[12];
-#pragma unroll
-        for (int ks = 0; ks < 12; ++ks) qc[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
-        f32x16 o[4] = {};
-        float rc = kUnset, sc = 0.0f;
-#pragma unroll 1
-        for (int kc0 = key0; kc0 < key1; kc0 += KT) {
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");       // no wave reads the tile before
-            stage(kc0, 0);
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
-            uint32_t found = 0;
-#pragma unroll 1
-            for (int i = lane * 16; i < 2 * S::plane; i += 1024) {
-                const uint4 y = *reinterpret_cast<const uint4*>(smem + S::value_at + i);
-                const uint32_t w4[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        if (cur.tiles > 0) look(key_of(cur, 0), off);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        int t = 0;
+        // (tiles of which no row of the wave sees any, here and at the end)
+        for (; t < t_begin && t < cur.tiles; ++t, off = after(off)) {
+            meet(t, off);
+            stage_ahead(t, off);
+        }
+        if (some > 0) {
+            begin_tile(t, off, true);
+            if constexpr (KB == 2) {
+                // tiles that are whole, as is the next, and the one to be staged
+                const int first = cur.down ? cur.tiles - whole : 0;
+                const int last = cur.down ? cur.tiles - 3 : min(whole - 2, (cur.key1 - cur.key0) / KT - 3);
+                while (t < first && t + 1 < t_end) {
+                    finish_tile(t, off, std::true_type{}, std::true_type{});
+                    ++t;
+                    off = after(off);
+                }
+                next_n = nope_at(cur, key_of(cur, t + 2));
+                next_r = rope_at(cur, key_of(cur, t + 2));
+                next_v = value_at(cur, key_of(cur, t + 2));
+                const int64_t step = cur.down ? -KT : KT;
+                step_n = step * kn_b;
+                step_r = step * kr_b;
+                step_v = step * vv_b;
+                while (t <= last) {
+                    finish_tile(t, off, std::true_type{}, std::false_type{});
+                    ++t;
+                    off = after(off);
+                }
+                while (t + 1 < t_end) {
+                    finish_tile(t, off, std::true_type{}, std::true_type{});
+                    ++t;
+                    off = after(off);
+                }
+                finish_tile(t, off, std::false_type{}, std::true_type{});
+            } else {
+                // (one key block: a tile begins and ends by itself)
+                while (true) {
+                    finish_tile(t, off, std::false_type{}, std::true_type{});
+                    if (t + 1 >= t_end) break;
+                    ++t;
+                    off = after(off);
+                    begin_tile(t, off, false);
+                }
             }
-            const bool odd = __ballot(found != 0) != 0;
+            ++t;
+            off = after(off);
+        } else if (more) {
+            load_queries(following);
+        }
+        for (; t < cur.tiles; ++t, off = after(off)) {
+            meet(t, off);
+            stage_ahead(t, off);
+        }
+        // Whether any wave wants the rows done over.
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const float total = sum_halves(sum[g]);
+            const int row = r0 + 32 * g + col;
+            careful = careful || __ballot(!(total < kMost && total > kLeast) && row < cur.q_rows && sees_of(cur, row) > cur.key0) != 0;
+        }
+        if (lane == 0) flags[S::buffers * NW + wave] = careful;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) any |= flags[S::buffers * NW + i];
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) == 0, 1)) {
+            // in the place of the last tile, which no wave reads any more (the other two
+            // are the next block's)
+#pragma unroll
+            for (int g = 0; g < G; ++g) put_rows(r0 + 32 * g, acc[g], ref[g], sum[g], smem + (S::listed ? after(after(off)) : 0) + wave * 32 * 256);
+            if (more && cur.tiles == 0) stage_first(following, off);
+        } else {
+            // careful_rows: 32 rows of a wave at a time, a tile at a time.
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");     // (of the next block's tiles)
 #pragma unroll 1
-            for (int b = 0; b < KB; ++b) {
-                f32x16 z = {};
+            for (int g = 0; g < G; ++g) {
+                const int x = r0 + 32 * g;
+                const int limit = sees_of(cur, x + col);
+                const int64_t qr = cur.q_row + min(x + col, cur.q_rows - 1);
+                const uint16_t* const qn_p = a.q_nope.data + qr * a.q_nope.stride_t + static_cast<int64_t>(cur.head) * a.q_nope.stride_h + 8 * half;
+                const uint16_t* const qr_p = a.q_rope.data + qr * a.q_rope.stride_t + static_cast<int64_t>(cur.head) * a.q_rope.stride_h + 8 * half;
+                bf16x8 qc[12];
 #pragma unroll
-                for (int ks = 0; ks < 12; ++ks)
-                    z = mfma(*reinterpret_cast<const bf16x8*>(smem + ka[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow), qc[ks], z);
-                const int seen_here = limit - kc0 - 32 * b - 4 * half;
-                float top = -INFINITY;
+                for (int ks = 0; ks < 12; ++ks) qc[ks] = *reinterpret_cast<const bf16x8*>(ks < 8 ? qn_p + 16 * ks : qr_p + 16 * (ks - 8));
+                f32x16 o[4] = {};
+                float rc = kUnset, sc = 0.0f;
+#pragma unroll 1
+                for (int kc0 = cur.key0; kc0 < cur.key1; kc0 += KT) {
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");       // no wave reads the tile before
+                    stage(cur, kc0, 0);
+                    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
+                    uint32_t found = 0;
+#pragma unroll 1
+                    for (int i = lane * 16; i < 2 * S::plane; i += 1024) {
+                        const uint4 y = *reinterpret_cast<const uint4*>(smem + S::value_at + i);
+                        const uint32_t w4[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    z[i] = (i & 3) + 8 * (i >> 2) < seen_here ? z[i] : -INFINITY;
-                    top = fmaxf(top, z[i]);
-                }
-                const float to = fminf(fmaxf(rc, max_halves(top) * c2), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
-                const float f = __builtin_amdgcn_exp2f(rc - to);
-                rc = to;
-                sc *= f;
-                uint32_t pairs[8];
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(z[i], c2, -rc)), e1 = __builtin_amdgcn_exp2f(fmaf(z[i + 1], c2, -rc));
-                    sc += e0;
-                    sc += e1;
-                    pairs[i >> 1] = kc::pack_bf16x2(e0, e1);
-                }
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[m][i] *= f;
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) {
-                        const uint8_t* at = smem + va[m & 1] + (m >> 1) * S::plane + (2 * b + ks) * 16 * kRow;
-                        const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
-                        const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kRow));
-                        i16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-                        // values that are not finite are left out of the product ...
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = (v[j] & 0x7F80) == 0x7F80 ? 0 : v[j];
-                        const u32x4 p4 = {pairs[4 * ks], pairs[4 * ks + 1], pairs[4 * ks + 2], pairs[4 * ks + 3]};
-                        o[m] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p4), o[m]);
+                        for (int j = 0; j < 4; ++j) found |= ((w4[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
                     }
-                }
-            }
-            // ... and added to the rows that see them, to which they give what they are
-            if (odd) {
+                    const bool odd = __ballot(found != 0) != 0;
 #pragma unroll 1
-                for (int j = 0; j < KT; ++j) {
+                    for (int b = 0; b < KB; ++b) {
+                        f32x16 z = {};
 #pragma unroll
-                    for (int m = 0; m < 4; ++m)
+                        for (int ks = 0; ks < 12; ++ks)
+                            z = mfma(*reinterpret_cast<const bf16x8*>(smem + ka[ks & 3] + (ks >> 2) * S::plane + b * 32 * kRow), qc[ks], z);
+                        const int seen_here = limit - kc0 - 32 * b - 4 * half;
+                        float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
-                            const uint32_t bits = *reinterpret_cast<const uint16_t*>(
-                                smem + S::value_at + (m >> 1) * S::plane + j * kRow + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
-                            o[m][i] += (bits & 0x7F80u) == 0x7F80u && kc0 + j < limit ? __uint_as_float(bits << 16) : 0.0f;
+                            z[i] = (i & 3) + 8 * (i >> 2) < seen_here ? z[i] : -INFINITY;
+                            top = fmaxf(top, z[i]);
                         }
+                        const float to = fminf(fmaxf(rc, max_halves(top) * c2), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
+                        const float f = __builtin_amdgcn_exp2f(rc - to);
+                        rc = to;
+                        sc *= f;
+                        uint32_t pairs[8];
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float e0 = __builtin_amdgcn_exp2f(fmaf(z[i], c2, -rc)), e1 = __builtin_amdgcn_exp2f(fmaf(z[i + 1], c2, -rc));
+                            sc += e0;
+                            sc += e1;
+                            pairs[i >> 1] = kc::pack_bf16x2(e0, e1);
+                        }
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[m][i] *= f;
+#pragma unroll
+                            for (int ks = 0; ks < 2; ++ks) {
+                                const uint8_t* at = smem + va[m & 1] + (m >> 1) * S::plane + (2 * b + ks) * 16 * kRow;
+                                const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
+                                const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 8 * kRow));
+                                i16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+                                // values that are not finite are left out of the product ...
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) v[j] = (v[j] & 0x7F80) == 0x7F80 ? 0 : v[j];
+                                const u32x4 p4 = {pairs[4 * ks], pairs[4 * ks + 1], pairs[4 * ks + 2], pairs[4 * ks + 3]};
+                                o[m] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p4), o[m]);
+                            }
+                        }
+                    }
+                    // ... and added to the rows that see them, to which they give what they are
+                    if (odd) {
+#pragma unroll 1
+                        for (int j = 0; j < KT; ++j) {
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const int c = 4 * (m & 1) + (i >> 2);       // 16 bytes of the row: channels 8c .. 8c + 7 of the plane
+                                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(
+                                        smem + S::value_at + (m >> 1) * S::plane + j * kRow + ((c ^ value_xor(j)) << 4) + 8 * half + 2 * (i & 3));
+                                    o[m][i] += (bits & 0x7F80u) == 0x7F80u && kc0 + j < limit ? __uint_as_float(bits << 16) : 0.0f;
+                                }
+                        }
+                    }
                 }
+                put_rows(x, o, rc, sc, smem + S::tile + wave * 32 * 256);
+            }
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");       // no wave reads the last tile
+                off = 0;
+                stage_first(following, off);
             }
         }
-        put_rows(x, o, rc, sc, smem + S::tile + wave * 32 * 256);
+        if (!more) return;
+        settle();
+        cur = following;
+        ++at;
     }
 }
 
@@ -767,11 +851,13 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
 }  // namespace
 
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(a.num_items) * static_cast<unsigned>(a.H));
+    const PrefillLists l = prefill_lists(a.num_items, a.H, a.rows);
+    const dim3 grid(l.lists > 0 ? static_cast<unsigned>(l.lists) * (a.H % 8 == 0 ? 8u : 1u)
+                                : static_cast<unsigned>(a.num_items) * static_cast<unsigned>(a.H));
     if (a.rows == 32)
         hipLaunchKernelGGL((prefill_kernel<1, 1, 32>), grid, dim3(64), 0, stream, a);
     else if (a.rows == 128)
-        hipLaunchKernelGGL((prefill_kernel<4, 1, 64>), grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((prefill_kernel<4, 1, 32>), grid, dim3(256), 0, stream, a);
     else if (a.rows == 256)
         hipLaunchKernelGGL((prefill_kernel<4, 2, 64>), grid, dim3(256), 0, stream, a);
     else

@@ -71,7 +71,7 @@ struct PrefillItem {
     int32_t key0, key1;
     int32_t seen0;
     int32_t part;       // partial block it writes; -1: the output itself
-    int32_t pad;
+    int32_t seq;        // the sequence (the planner's own use)
 };
 // The merge of a block's partials, part0 .. part0 + num_parts - 1.
 struct PrefillMerge {
@@ -81,6 +81,22 @@ struct PrefillMerge {
     int32_t pad[2];
 };
 constexpr int kPrefillRecordInts = 8;
+// Behind the records, where workgroups go through several items each (256 rows):
+// int32 first[lists + 1], then the lists' entries, x = local head + heads * item (or
+// ~x: the block's tiles are gone through from the last to the first), where
+// a list is gone through by one workgroup on each XCD, for the heads of that XCD
+// (heads = H / 8), or by one workgroup (heads = H) if the heads do not divide by 8.
+constexpr int kListedRows = 256;
+struct PrefillLists {
+    int32_t lists, heads;
+    int64_t entries;
+};
+inline PrefillLists prefill_lists(int64_t num_items, int32_t H, int32_t rows) {
+    if (rows != kListedRows) return {0, 0, 0};
+    const int32_t heads = H % 8 == 0 ? H / 8 : H, most = H % 8 == 0 ? 32 : 256;
+    const int64_t entries = num_items * heads;
+    return {static_cast<int32_t>(entries < most ? entries : most), heads, entries};
+}
 static_assert(sizeof(PrefillItem) == 4 * kPrefillRecordInts && sizeof(PrefillMerge) == sizeof(PrefillItem), "one record size");
 
 constexpr int kNope = 128, kValue = 128;    // channels of a head's expanded keys and values
@@ -95,6 +111,7 @@ struct HeadRows {
 struct PrefillArgs {
     const PrefillItem* items;
     const PrefillMerge* merges;
+    const int32_t* first;       // lists (prefill_lists); null: an item of one head per workgroup
     int32_t num_items, num_merges, num_parts, H;
     int32_t rows;               // query rows of a workgroup: 32 per wave
     int32_t total_q, total_kv;
@@ -110,6 +127,11 @@ struct PrefillArgs {
 
 constexpr int kRowsPerWave = 32;
 constexpr int64_t kPartRowBytes = kValue * 4 + 2 * 4;
+
+// For tests and measurements of one shape (exported, not part of the public ABI):
+// the calling thread's plans take workgroups of `rows` query rows (32, 128 or
+// 256); 0: as the planner chooses.
+extern "C" void mla_internal_prefill_rows(int32_t rows);
 
 hipError_t launch_norm_rope_append(const NormRopeArgs& a, bool lowbit, hipStream_t stream);
 hipError_t launch_rope_queries(const RopeArgs& a, hipStream_t stream);

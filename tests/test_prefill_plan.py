@@ -41,14 +41,38 @@ PLANS = [
     ([1], [1], 1, True), ([64], [64], 16, True), ([1000, 3, 129], [1000, 70, 5000], 4, True),
     ([5, 0, 3], [2, 0, 0], 2, True), ([200], [100], 3, True), ([7], [30000], 2, True), ([300], [20000], 1, False),
     ([1] * 40, list(range(0, 4000, 100)), 8, True), ([257, 31], [0, 900], 16, False), ([], [], 1, True),
-    ([1, 1], [100000, 3], 16, True),
+    ([1, 1], [100000, 3], 16, True), ([1500, 700, 3000, 20], [1500, 700, 3000, 20], 64, True),
+    ([256] * 70, [300] * 70, 3, False), ([2000, 0, 900], [0, 400, 50], 24, True),
 ]
+
+
+def check_order(items, work, rest, info, H):
+    """Items the longest first; blocks of 256 rows sequence by sequence, and dealt out to lists."""
+    if info.rows != 256:
+        assert work == sorted(work, reverse=True) and len(rest) == 0
+        return
+    seqs = items[:, 7].tolist()
+    runs = [i for i in range(len(seqs)) if i == 0 or seqs[i] != seqs[i - 1]]
+    assert len(runs) == len(set(seqs))
+    for a, b in zip(runs, runs[1:] + [len(seqs)]):
+        assert work[a:b] == sorted(work[a:b], reverse=True)
+    heads, most = (H // 8, 32) if H % 8 == 0 else (H, 256)
+    lists = min(most, heads * len(items))
+    first, entries = rest[:lists + 1], rest[lists + 1:]
+    entries = np.where(entries < 0, ~entries, entries)          # (complement: from the last tile down)
+    assert first[0] == 0 and first[-1] == len(entries) and (np.diff(first) > 0).all()
+    assert sorted(entries.tolist()) == list(range(heads * len(items)))
+    # taken as they come: no list waits longer than its last entry
+    load = [sum(5 + work[e // heads] for e in entries[a:b]) for a, b in zip(first, first[1:])]
+    last = [5 + work[entries[b - 1] // heads] for b in first[1:]]
+    assert all(n - t <= min(load) for n, t in zip(load, last))
 
 
 @pytest.mark.parametrize("q,kv,H,causal", PLANS)
 def test_plan_covers_every_pair_once(mp, q, kv, H, causal):
     plan, info = mp.mla_plan_prefill(q, kv, H, causal)
-    rec = plan.reshape(-1, 8)
+    records = 8 * (info.num_items + info.num_merges)
+    rec = plan[:records].reshape(-1, 8)
     items, merges = rec[:info.num_items], rec[info.num_items:]
     assert info.total_q == sum(q) and info.total_kv == sum(kv) and len(merges) == info.num_merges
     q0, k0 = np.cumsum([0] + list(q)), np.cumsum([0] + list(kv))
@@ -67,7 +91,7 @@ def test_plan_covers_every_pair_once(mp, q, kv, H, causal):
             lo, hi = key0, max(key0, min(key1, seen0 + r))
             assert hi <= max(limit, key0)
             reach[q_row + r].append((lo, hi, limit))
-    assert work == sorted(work, reverse=True)
+    check_order(items, work, plan[records:], info, H)
     for spans in reach:
         spans.sort()
         assert spans
@@ -121,9 +145,13 @@ def test_plan_capacity_and_nulls(mp):
     q = np.array([200], np.int32)
     buf = np.zeros(64, np.int32)
     p, i = q.ctypes.data, ctypes.byref(info)
-    assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, buf.ctypes.data, 15, i) == 1
-    assert info.plan_ints == 16 and not buf.any()
-    assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, buf.ctypes.data, 16, i) == 0
+    assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, None, 0, i) == 0
+    n = info.plan_ints
+    assert 8 <= n < 64
+    assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, buf.ctypes.data, n - 1, i) == 1
+    assert info.plan_ints == n and not buf.any()
+    assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, buf.ctypes.data, n, i) == 0
+    assert buf[:n].any() and not buf[n:].any()
     assert lib.mla_plan_prefill(p, p, None, None, 1, 2, 1, None, 0, None) == 1
     assert lib.mla_plan_prefill(None, p, None, None, 1, 2, 1, None, 0, i) == 1
     assert lib.mla_plan_prefill(p, p, None, None, -1, 2, 1, None, 0, i) == 1
