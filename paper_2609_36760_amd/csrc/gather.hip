@@ -17,16 +17,20 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRopeRows = 8;        // of a RoPE wave
+constexpr int kManyRows = 16384;
 
-// Sequence of output row r: how many of cu_rows[1 .. B] are at or below it
-// (r uniform in the wave; B at the rows behind the last sequence).
-__device__ __forceinline__ int sequence_of(const GatherArgs& a, int r, int lane) {
-    int b = 0;
+// Sequences of the output rows first .. first + N - 1 (uniform in the wave): how
+// many of cu_rows[1 .. B] are at or below each (B at the rows behind the last
+// sequence).
+template <int N>
+__device__ __forceinline__ void sequences_of(const GatherArgs& a, int first, int lane, int (&b)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) b[k] = 0;
     for (int i = 0; i < a.B; i += 64) {
         const int c = i + lane < a.B ? a.cu_rows[1 + i + lane] : INT32_MAX;
-        b += __popcll(__ballot(c <= r));
+#pragma unroll
+        for (int k = 0; k < N; ++k) b[k] += __popcll(__ballot(c <= first + k));
     }
-    return b;
 }
 
 // Where a token is: a BF16 row, or offset `off` of a packed page.
@@ -112,35 +116,33 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(GatherArgs a) {
     const uint32_t content_waves = (static_cast<uint32_t>(a.n) + kRows - 1) / kRows;
     if (wave < content_waves) {
         const int first = static_cast<int>(wave) * kRows;
-        uint4 x[kRows];
-        bool there[kRows];
+        int b[kRows];
+        sequences_of(a, first, lane, b);
+        // (rows behind the last sequence read as its last row, and are not written)
+        Source s[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int b = sequence_of(a, first + i, lane);
-            there[i] = first + i < a.n && b < a.B;
-            if (there[i]) x[i] = read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, first + i), false, lane);
-        }
+        for (int i = 0; i < kRows; ++i) s[i] = source_of<CBITS == 16, kProt>(a, min(b[i], a.B - 1), first + i);
+        uint4 x[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) x[i] = read<CBITS, kPaper>(a, s[i], false, lane);
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
-            if (there[i]) *reinterpret_cast<uint4*>(a.c_out + static_cast<int64_t>(first + i) * a.c_out_stride + lane * 8) = x[i];
+            if (first + i < a.n && b[i] < a.B) *reinterpret_cast<uint4*>(a.c_out + static_cast<int64_t>(first + i) * a.c_out_stride + lane * 8) = x[i];
         return;
     }
     const int first = static_cast<int>(wave - content_waves) * kRopeRows;
     const int r = first + (lane >> 3);
-    int b = a.B;
+    int all[kRopeRows], b = a.B;
+    sequences_of(a, first, lane, all);
 #pragma unroll
-    for (int i = 0; i < kRopeRows; ++i) {
-        const int bi = sequence_of(a, first + i, lane);
-        if ((lane >> 3) == i) b = bi;
-    }
+    for (int i = 0; i < kRopeRows; ++i) b = (lane >> 3) == i ? all[i] : b;
     if (r >= a.n || b >= a.B) return;
     const uint4 x = read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, r), true, lane);
     *reinterpret_cast<uint4*>(a.k_out + static_cast<int64_t>(r) * a.k_out_stride + (lane & 7) * 8) = x;
 }
 
-template <int CBITS, bool kProt, bool kPaper>
-hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
-    constexpr int kRows = 1;
+template <int CBITS, bool kProt, bool kPaper, int kRows>
+hipError_t launch_rows(const GatherArgs& a, hipStream_t stream) {
     const int64_t n = a.n;
     const int64_t waves = (n + kRows - 1) / kRows + (n + kRopeRows - 1) / kRopeRows;
     static_assert((kMaxAppendTokens + kMaxAppendTokens / kRopeRows + 1) * 64 + kThreads <= kMaxDispatchItems, "launch size");
@@ -148,6 +150,14 @@ hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((gather_kernel<CBITS, kProt, kPaper, kRows>), dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0,
                        stream, a);
     return hipGetLastError();
+}
+template <int CBITS, bool kProt, bool kPaper>
+hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
+    // Four rows per wave overlap their chains of loads (row -> page -> codes), where there
+    // are waves enough for the card all the same (128K rows, 4 bits: 40 us against 49;
+    // 32K: 13.7 against 15.8; at 16K and below no difference).
+    if (a.n >= kManyRows) return launch_rows<CBITS, kProt, kPaper, 4>(a, stream);
+    return launch_rows<CBITS, kProt, kPaper, 1>(a, stream);
 }
 
 }  // namespace
