@@ -186,6 +186,7 @@ typedef struct mla_prefill_plan {
     int32_t num_items;          /* work items per head                          */
     int32_t num_merges;         /* row blocks whose keys are split              */
     int32_t num_parts;          /* partial row blocks per head                  */
+    int32_t part_rows;          /* rows of a partial block                      */
 } mla_prefill_plan;
 int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_t* q_starts,
                      const int32_t* kv_starts, int32_t B, int32_t H, int32_t causal,

@@ -40,7 +40,7 @@ class mla_prefill_plan(ctypes.Structure):
     _fields_ = [("plan_ints", ctypes.c_int64), ("workspace_bytes", ctypes.c_int64), ("total_q", ctypes.c_int64),
                 ("total_kv", ctypes.c_int64), ("B", ctypes.c_int32), ("H", ctypes.c_int32),
                 ("causal", ctypes.c_int32), ("rows", ctypes.c_int32), ("num_items", ctypes.c_int32),
-                ("num_merges", ctypes.c_int32), ("num_parts", ctypes.c_int32)]
+                ("num_merges", ctypes.c_int32), ("num_parts", ctypes.c_int32), ("part_rows", ctypes.c_int32)]
 
 
 class mla_head_rows(ctypes.Structure):

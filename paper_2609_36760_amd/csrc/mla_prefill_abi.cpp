@@ -157,16 +157,18 @@ int32_t splits_of(int32_t tiles, int64_t most) {
 struct Shape {
     int32_t rows, slots, least_tiles;
 };
-constexpr Shape kShapes[] = {{32, 512, 4}, {128, 512, 8}, {256, 256, 8}};
+constexpr Shape kShapes[] = {{128, 512, 4}, {256, 256, 8}};
 
-thread_local int32_t g_rows = 0;       // mla_internal_prefill_rows
-
+// Up to 128 rows per sequence the reads of the keys bound the kernel, and two small
+// workgroups per CU overlap each other's beginnings and ends; beyond, a workgroup of
+// 256 rows reads the keys half as often.  Measured, 128 rows / 256 rows: 256 prompts
+// of 64, 64 heads 283 / 575 us; 128 of 128 290 / 398; 64 of 256 391 / 351; 129
+// rows on 16 x 4096 keys 878 / 548; 16 of 1024 734 / 588.  (Workgroups of one wave and
+// 32 rows took as long as 128 rows from 1 to 32 rows, 24 x 2K keys: 154 / 146 us.)
 Shape choose_rows(const Lengths& n) {
-    for (const Shape& s : kShapes)
-        if (s.rows == g_rows) return s;
     int32_t most = 0;
     for (int32_t b = 0; b < n.B; ++b) most = std::max(most, n.q[b]);
-    return most <= 32 ? kShapes[0] : most <= 128 ? kShapes[1] : kShapes[2];
+    return most <= kShapes[0].rows ? kShapes[0] : kShapes[1];
 }
 
 int check_lengths(const Lengths& n, int64_t* total_q, int64_t* total_kv) {
@@ -289,10 +291,6 @@ bool rows_apart(int64_t stride_t, int64_t stride_h, int64_t T, int64_t H, int64_
 }
 
 }  // namespace
-
-namespace mla {
-extern "C" void mla_internal_prefill_rows(int32_t rows) { g_rows = rows; }
-}  // namespace mla
 
 extern "C" {
 
@@ -432,12 +430,14 @@ int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_
     const int64_t most = std::max<int64_t>(
         shape.least_tiles, static_cast<int64_t>(std::ceil(static_cast<double>(tiles) * H / shape.slots)));
     int64_t items = 0, merges = 0, parts = 0;
-    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t, int32_t, int32_t key1, int32_t) {
+    int32_t part_rows = 0;
+    each_block(n, shape.rows, [&](int32_t, int32_t, int32_t rows, int32_t, int32_t key1, int32_t) {
         const int32_t s = splits_of(tiles_of(key1), most);
         items += s;
         if (s > 1) {
             ++merges;
             parts += s;
+            part_rows = std::max(part_rows, rows);
         }
     });
     // launches of one dispatch: 2 threads per row of an item, one wave per merged row
@@ -452,7 +452,8 @@ int mla_plan_prefill(const int32_t* q_lens, const int32_t* kv_lens, const int32_
     p.num_merges = static_cast<int32_t>(merges);
     p.num_parts = static_cast<int32_t>(parts);
     p.plan_ints = plan_ints(p);
-    p.workspace_bytes = parts * H * shape.rows * mla::kPartRowBytes;
+    p.part_rows = part_rows;
+    p.workspace_bytes = parts * H * part_rows * mla::kPartRowBytes;
     *info = p;
     if (plan == nullptr) return MLA_OK;
     if (plan_capacity < p.plan_ints) return MLA_EINVAL;
@@ -513,7 +514,8 @@ int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan, const ml
     if (static_cast<int64_t>(info->num_items) * info->H > mla::kMaxDispatchItems / (2 * info->rows) - 8 ||
         static_cast<int64_t>(info->num_merges) * info->H > mla::kMaxDispatchItems / 64 / info->rows)
         return MLA_ENOTSUP;
-    const int64_t part_rows = static_cast<int64_t>(info->num_parts) * info->H * info->rows;
+    if (info->part_rows < 0 || info->part_rows > info->rows || (info->num_merges > 0 && info->part_rows == 0)) return MLA_EINVAL;
+    const int64_t part_rows = static_cast<int64_t>(info->num_parts) * info->H * info->part_rows;
     if (info->workspace_bytes != part_rows * mla::kPartRowBytes) return MLA_EINVAL;
     if (plan == nullptr || out == nullptr) return MLA_EINVAL;
     if (!aligned(plan, 16) || !aligned(out, 16)) return MLA_ENOTSUP;
@@ -545,6 +547,7 @@ int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan, const ml
     a.num_parts = info->num_parts;
     a.H = info->H;
     a.rows = info->rows;
+    a.part_rows = info->part_rows;
     a.total_q = static_cast<int32_t>(info->total_q);
     a.total_kv = static_cast<int32_t>(info->total_kv);
     a.scale_log2 = softmax_scale * 1.4426950408889634f;

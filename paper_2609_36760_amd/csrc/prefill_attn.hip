@@ -584,8 +584,8 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int r = x + col;
         if (cur.part >= 0) {
-            if (r >= cur.q_rows) return;
-            const int64_t row = (static_cast<int64_t>(cur.part) * a.H + cur.head) * S::rows + r;
+            if (r >= min(cur.q_rows, a.part_rows)) return;
+            const int64_t row = (static_cast<int64_t>(cur.part) * a.H + cur.head) * a.part_rows + r;
             float* to = a.part_o + row * kValue + 4 * half;
 #pragma unroll
             for (int m = 0; m < 4; ++m)
@@ -830,15 +830,15 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
 __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     const uint32_t w = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const uint32_t per_block = static_cast<uint32_t>(a.H) * a.rows;
+    const uint32_t per_block = static_cast<uint32_t>(a.H) * a.part_rows;
     const uint32_t id = w / per_block, rest = w - id * per_block;
     if (id >= static_cast<uint32_t>(a.num_merges)) return;
-    const int head = static_cast<int>(rest / a.rows), r = static_cast<int>(rest % a.rows);
+    const int head = static_cast<int>(rest / a.part_rows), r = static_cast<int>(rest % a.part_rows);
     const PrefillMerge g = a.merges[id];
     if (r >= g.q_rows || g.q_row < 0 || g.q_row + r >= a.total_q) return;
     const int part0 = max(g.part0, 0), parts = min(g.num_parts, a.num_parts - part0);
-    const int64_t step = static_cast<int64_t>(a.H) * a.rows;
-    const int64_t row = part0 * step + static_cast<int64_t>(head) * a.rows + r;
+    const int64_t step = static_cast<int64_t>(a.H) * a.part_rows;
+    const int64_t row = part0 * step + static_cast<int64_t>(head) * a.part_rows + r;
     float top = kUnset;
     for (int j = 0; j < parts; ++j) top = fmaxf(top, a.part_m[row + j * step]);
     float sum = 0.0f;
@@ -866,9 +866,7 @@ hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
     const PrefillLists l = prefill_lists(a.num_items, a.H, a.rows);
     const dim3 grid(l.lists > 0 ? static_cast<unsigned>(l.lists) * (a.H % 8 == 0 ? 8u : 1u)
                                 : static_cast<unsigned>(a.num_items) * static_cast<unsigned>(a.H));
-    if (a.rows == 32)
-        hipLaunchKernelGGL((prefill_kernel<1, 1, 32>), grid, dim3(64), 0, stream, a);
-    else if (a.rows == 128)
+    if (a.rows == 128)
         hipLaunchKernelGGL((prefill_kernel<4, 1, 32>), grid, dim3(256), 0, stream, a);
     else if (a.rows == 256)
         hipLaunchKernelGGL((prefill_kernel<4, 2, 64>), grid, dim3(256), 0, stream, a);
@@ -876,7 +874,7 @@ hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
         return hipErrorInvalidValue;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.num_merges == 0) return e;
-    const int64_t waves = static_cast<int64_t>(a.num_merges) * a.H * a.rows;
+    const int64_t waves = static_cast<int64_t>(a.num_merges) * a.H * a.part_rows;
     hipLaunchKernelGGL(prefill_merge_kernel, dim3(static_cast<unsigned>((waves + 3) / 4)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }

@@ -113,25 +113,21 @@ struct PrefillArgs {
     const PrefillMerge* merges;
     const int32_t* first;       // lists (prefill_lists); null: an item of one head per workgroup
     int32_t num_items, num_merges, num_parts, H;
-    int32_t rows;               // query rows of a workgroup: 32 per wave
+    int32_t rows;               // query rows of a workgroup
+    int32_t part_rows;          // rows of a partial block: the most that a block with split keys has
     int32_t total_q, total_kv;
     HeadRows q_nope, q_rope, k_nope, k_rope, v;
     float scale_log2;           // softmax_scale * log2(e)
     uint16_t* out;
     int64_t out_stride_t, out_stride_h;
     float* lse;
-    float* part_m;              // [num_parts][H][rows], log2 units
+    float* part_m;              // [num_parts][H][part_rows], log2 units
     float* part_l;
-    float* part_o;              // [num_parts][H][rows][128], normalized
+    float* part_o;              // [num_parts][H][part_rows][128], normalized
 };
 
 constexpr int kRowsPerWave = 32;
 constexpr int64_t kPartRowBytes = kValue * 4 + 2 * 4;
-
-// For tests and measurements of one shape (exported, not part of the public ABI):
-// the calling thread's plans take workgroups of `rows` query rows (32, 128 or
-// 256); 0: as the planner chooses.
-extern "C" void mla_internal_prefill_rows(int32_t rows);
 
 hipError_t launch_norm_rope_append(const NormRopeArgs& a, bool lowbit, hipStream_t stream);
 hipError_t launch_rope_queries(const RopeArgs& a, hipStream_t stream);

@@ -114,7 +114,8 @@ def test_plan_covers_every_pair_once(mp, q, kv, H, causal):
         assert owner[p][:2] == block and owner[p][2] == kv[seq_of[block[0]]]
     whole = [int(x[0]) for x in items if x[6] < 0]
     assert len(set(whole)) == len(whole) and not set(whole) & {int(x[0]) for x in merges}
-    assert info.workspace_bytes == info.num_parts * H * info.rows * (128 * 4 + 8)
+    assert info.part_rows == max((m[1] for m in merges.tolist()), default=0)
+    assert info.workspace_bytes == info.num_parts * H * info.part_rows * (128 * 4 + 8)
 
 
 def test_plan_starts(mp):
@@ -183,7 +184,7 @@ def _attn(mp, q=(40,), kv=(5000,), H=2, info_over=None, **over):
     (dict(k_rope=(None, 64, 0)), 1), (dict(k_rope=(4096, 60, 0)), 2),
     (dict(out_t=128, out_h=128), 1), (dict(out_t=256, out_h=64), 1), (dict(out_t=-256), 1), (dict(out_t=260), 2),
     (dict(workspace=None), 1), (dict(size=0), 1), (dict(workspace=264), 2),
-    (dict(info_over=dict(rows=64)), 1), (dict(info_over=dict(rows=0)), 1), (dict(info_over=dict(H=0)), 1),
+    (dict(info_over=dict(rows=64)), 1), (dict(info_over=dict(part_rows=0)), 1), (dict(info_over=dict(part_rows=129)), 1), (dict(info_over=dict(rows=0)), 1), (dict(info_over=dict(H=0)), 1),
     (dict(info_over=dict(plan_ints=8)), 1), (dict(info_over=dict(num_items=-1)), 1), (dict(info_over=dict(total_q=0)), 1),
     (dict(info_over=dict(workspace_bytes=0)), 1), (dict(info_over=dict(total_kv=1 << 31)), 1),
 ])
