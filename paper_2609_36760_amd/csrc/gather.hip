@@ -2,8 +2,9 @@
 // a token become bf16(scale * (q - zero)), the product rounded to fp32 first;
 // BF16 rows (the BF16 cache, protected tokens) are copied bit for bit.
 //
-// A wave takes the 512 content channels of kRows output rows (64 lanes x 8
-// channels: one 4-bit code word in, 16 bytes out), or the RoPE keys of 8 rows.
+// A wave takes the 512 content channels of an output row (64 lanes x 8 channels:
+// one 4-bit code word in, 16 bytes out) or the RoPE keys of 8 rows, or, of many rows,
+// both of 8.
 // The bytes written are three times the bytes read, so the work split follows
 // the output: every store instruction writes whole rows.
 #include <hip/hip_runtime.h>
@@ -108,43 +109,72 @@ __device__ __forceinline__ uint4 read(const GatherArgs& a, const Source& s, bool
         return values<2>(*reinterpret_cast<const uint32_t*>(s.page + s.off * 128 + (lane >> 1) * 4), 8 * (lane & 1), scale, zero);
 }
 
-// CBITS 16: the BF16 cache.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// kStream: past the caches, as rows that a product reads later, many at a time.
+template <bool kStream>
+__device__ __forceinline__ void put(uint16_t* to, const uint4& x) {
+    if constexpr (kStream) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), reinterpret_cast<u32x4*>(to));
+    else *reinterpret_cast<uint4*>(to) = x;
+}
+
+// kRows consecutive rows of a wave; a single row's RoPE keys are left to waves of
+// their own, behind the others.  CBITS 16: the BF16 cache.
 template <int CBITS, bool kProt, bool kPaper, int kRows>
 __global__ __launch_bounds__(kThreads) void gather_kernel(GatherArgs a) {
+    static_assert(kRows == 1 || kRows == kRopeRows, "8 lanes per RoPE key");
+    constexpr bool kStream = kRows > 1;
     const int lane = static_cast<int>(threadIdx.x & 63);
     const uint32_t wave = __builtin_amdgcn_readfirstlane((blockIdx.x * kThreads + threadIdx.x) >> 6);
     const uint32_t content_waves = (static_cast<uint32_t>(a.n) + kRows - 1) / kRows;
-    if (wave < content_waves) {
+    const bool content = wave < content_waves;
+    if (content) {
         const int first = static_cast<int>(wave) * kRows;
         int b[kRows];
         sequences_of(a, first, lane, b);
-        // (rows behind the last sequence read as its last row, and are not written)
+        // (rows behind the last sequence read as if they were the last one's, and are not
+        // written)
         Source s[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) s[i] = source_of<CBITS == 16, kProt>(a, min(b[i], a.B - 1), first + i);
         uint4 x[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) x[i] = read<CBITS, kPaper>(a, s[i], false, lane);
+        if constexpr (kRows > 1) {
+            const int mine = lane >> 3;
+            Source t = s[0];
+            bool there = b[0] < a.B;
+#pragma unroll
+            for (int i = 1; i < kRows; ++i) {
+                t.row = mine == i ? s[i].row : t.row;
+                t.page = mine == i ? s[i].page : t.page;
+                t.off = mine == i ? s[i].off : t.off;
+                there = mine == i ? b[i] < a.B : there;
+            }
+            const uint4 k = read<CBITS, kPaper>(a, t, true, lane);
+            if (first + mine < a.n && there) put<kStream>(a.k_out + static_cast<int64_t>(first + mine) * a.k_out_stride + (lane & 7) * 8, k);
+        }
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
-            if (first + i < a.n && b[i] < a.B) *reinterpret_cast<uint4*>(a.c_out + static_cast<int64_t>(first + i) * a.c_out_stride + lane * 8) = x[i];
-        return;
+            if (first + i < a.n && b[i] < a.B) put<kStream>(a.c_out + static_cast<int64_t>(first + i) * a.c_out_stride + lane * 8, x[i]);
     }
-    const int first = static_cast<int>(wave - content_waves) * kRopeRows;
-    const int r = first + (lane >> 3);
-    int all[kRopeRows], b = a.B;
-    sequences_of(a, first, lane, all);
+    if constexpr (kRows == 1) {
+        if (content) return;
+        const int first = static_cast<int>(wave - content_waves) * kRopeRows;
+        const int r = first + (lane >> 3);
+        int all[kRopeRows], b = a.B;
+        sequences_of(a, first, lane, all);
 #pragma unroll
-    for (int i = 0; i < kRopeRows; ++i) b = (lane >> 3) == i ? all[i] : b;
-    if (r >= a.n || b >= a.B) return;
-    const uint4 x = read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, r), true, lane);
-    *reinterpret_cast<uint4*>(a.k_out + static_cast<int64_t>(r) * a.k_out_stride + (lane & 7) * 8) = x;
+        for (int i = 0; i < kRopeRows; ++i) b = (lane >> 3) == i ? all[i] : b;
+        if (r >= a.n || b >= a.B) return;
+        put<kStream>(a.k_out + static_cast<int64_t>(r) * a.k_out_stride + (lane & 7) * 8,
+                     read<CBITS, kPaper>(a, source_of<CBITS == 16, kProt>(a, b, r), true, lane));
+    }
 }
 
 template <int CBITS, bool kProt, bool kPaper, int kRows>
 hipError_t launch_rows(const GatherArgs& a, hipStream_t stream) {
     const int64_t n = a.n;
-    const int64_t waves = (n + kRows - 1) / kRows + (n + kRopeRows - 1) / kRopeRows;
+    const int64_t waves = (n + kRows - 1) / kRows + (kRows == 1 ? (n + kRopeRows - 1) / kRopeRows : 0);
     static_assert((kMaxAppendTokens + kMaxAppendTokens / kRopeRows + 1) * 64 + kThreads <= kMaxDispatchItems, "launch size");
     const int64_t groups = (waves * 64 + kThreads - 1) / kThreads;
     hipLaunchKernelGGL((gather_kernel<CBITS, kProt, kPaper, kRows>), dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0,
@@ -153,10 +183,10 @@ hipError_t launch_rows(const GatherArgs& a, hipStream_t stream) {
 }
 template <int CBITS, bool kProt, bool kPaper>
 hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
-    // Four rows per wave overlap their chains of loads (row -> page -> codes), where there
-    // are waves enough for the card all the same (128K rows, 4 bits: 40 us against 49;
-    // 32K: 13.7 against 15.8; at 16K and below no difference).
-    if (a.n >= kManyRows) return launch_rows<CBITS, kProt, kPaper, 4>(a, stream);
+    // Eight rows per wave overlap their chains of loads (row -> page -> codes) and share
+    // the search and the RoPE keys' wave, where there are waves enough for the card all
+    // the same.
+    if (a.n >= kManyRows) return launch_rows<CBITS, kProt, kPaper, kRopeRows>(a, stream);
     return launch_rows<CBITS, kProt, kPaper, 1>(a, stream);
 }
 
