@@ -100,6 +100,45 @@ def test_against_64_bits(case):
     c.check(str(CASES[case][:2])[:60])
 
 
+def directions(c):
+    """Directions of the plan's list entries: up, and down from the last tile."""
+    n = c.info.num_items
+    lists = min(32, n * (c.H // 8))
+    entries = c.plan[8 * (n + c.info.num_merges) + lists + 1:]
+    return int((entries >= 0).sum()), int((entries < 0).sum())
+
+
+@pytest.mark.parametrize("q,kv,H,heads", [
+    ([6500], [6500], 64, [0, 9, 15, 63]),               # blocks that go up and blocks that go down
+    ([300, 0, 900, 257, 64, 1], [300, 70, 0, 600, 6300, 65], 128, [0, 1, 127]),     # without rows, without keys
+    ([1030] * 5, [1500, 3, 1030, 700, 6200], 40, [0, 4, 39]),
+])
+def test_lists_of_blocks(q, kv, H, heads):
+    """Workgroups that go through several blocks each, of one sequence and another."""
+    c = Call(q, kv, H, True, seed=11)
+    if len(q) == 1:
+        assert min(directions(c)) > 0
+    c.run()
+    c.check(f"lists {q[:3]}", heads)
+
+
+@pytest.mark.parametrize("q,kv", [([1600], [7000]), ([600, 500, 300], [600, 900, 300])])
+def test_blocks_done_over_between_others(q, kv):
+    """Heads whose scores outgrow the first keys', whose first keys stand far above the others (a visible row's sum
+    vanishes beside a hidden key), or whose hidden values are not finite, beside heads that are ordinary."""
+    c = Call(q, kv, 128, True, seed=12)
+    if len(q) == 1:
+        assert min(directions(c)) > 0
+    nk, nq = kv[0], q[0]
+    c.k_nope[nk // 2:nk, 3] *= 40.0                     # scores up to 40 tau 11 |N(0, 1)|, well above e^60
+    c.q_nope[:nq, 3] *= 4.0
+    c.k_nope[nk - 20:nk, 7] *= 40.0                     # seen by few rows
+    c.q_nope[:nq, 7] *= 4.0
+    c.v[nk - 40, 9], c.v[nk - 1, 17, 5] = float("nan"), float("inf")
+    c.run()
+    c.check("done over", [0, 3, 7, 9, 17, 18, 127])
+
+
 @pytest.mark.parametrize("layout", ["heads", "shared"])
 @pytest.mark.parametrize("q,kv,causal", [([65, 7], [100, 300], True), ([2, 1], [700, 3000], False)])
 def test_layouts(layout, q, kv, causal):

@@ -299,6 +299,43 @@ def test_large_prompt_equals_its_parts():
     assert torch.equal(whole.cache, parts.cache) and torch.equal(whole.prot, parts.prot)
 
 
+@pytest.mark.parametrize("kind,prot", [(k, None) for k in KINDS] + [(k, (4, 128)) for k in KINDS[:4]])
+def test_many_tokens_equal_their_parts(kind, prot):
+    """16 400 tokens and more in one call (several per wave) write and read what calls over their parts do, which the
+    tests above compare with the oracle; rows behind the last sequence stay."""
+    import torch
+    first, lens = [0, 7, 0, 2900, 1, 0, 5, 0], [2999, 2811, 2900, 2901, 1, 2950, 2700, 2998]
+    whole, parts = (Batch(first, lens, kind, seed=9, prot=prot) for _ in range(2))
+    assert whole.n > 16384 and whole.n % 2 == 1
+    whole.append()
+    whole.gather(n=whole.n + 21)
+    c_out, k_out = torch.empty_like(whole.c_out), torch.empty_like(whole.k_out)
+    c_read, k_read = torch.full_like(whole.c_read, 9.0), torch.full_like(whole.k_read, 9.0)
+    mp, d = parts.mp, parts.dev
+    lens_d = d(np.asarray(lens, np.int32))
+    for b in range(len(lens)):
+        a, e = int(parts.cu[b]), int(parts.cu[b + 1])
+        head = (mp.rms_norm(EPS, parts.w), mp.rotation(parts.rotary), parts.x[a:e], parts.k[a:e], d(parts.pos[a:e]),
+                d(parts.slots[a:e]), parts.cache, parts.num_pages)
+        read = (parts.cache, parts.num_pages, d(parts.table[b:b + 1]), d(np.array([0, e - a], np.int32)))
+        to = dict(c_out=c_out[a:e], k_out=k_out[a:e])
+        at = (c_read[a:e], k_read[a:e], d(np.array(first[b:b + 1], np.int32)))
+        if prot is not None:
+            mp.mla_lowbit_norm_rope_append_protected(parts.fmt, parts.policy, *head, d(parts.seq[a:e]), lens_d,
+                                                     d(parts.prot_slot), parts.prot, parts.num_prot, **to)
+            mp.mla_lowbit_gather_protected(parts.fmt, parts.policy, *read, lens_d[b:b + 1], parts.prot, parts.num_prot,
+                                           d(parts.prot_slot[b:b + 1]), *at)
+        else:
+            (mp.mla_bf16_norm_rope_append if parts.bf16 else mp.mla_lowbit_norm_rope_append)(parts.fmt, *head, **to)
+            (mp.mla_bf16_gather if parts.bf16 else mp.mla_lowbit_gather)(parts.fmt, *read, *at)
+    torch.cuda.synchronize()
+    assert torch.equal(whole.cache, parts.cache), "cache bytes"
+    assert prot is None or torch.equal(whole.prot, parts.prot), "protection rows"
+    for got, want, what in ((whole.c_out, c_out, "latents"), (whole.k_out, k_out, "keys"),
+                            (whole.c_read, c_read, "latents read back"), (whole.k_read, k_read, "keys read back")):
+        assert torch.equal(got, want), what
+
+
 @pytest.mark.parametrize("n,H", [(1, 1), (3, 16), (77, 5), (1000, 128)])
 @pytest.mark.parametrize("halves", [False, True])
 @pytest.mark.parametrize("how", ["out", "in place", "heads"])
