@@ -210,8 +210,8 @@ typedef struct mla_head_rows {
  *   workspace  device, 256-byte aligned, workspace_bytes (at least
  *              info->workspace_bytes); calls that may overlap need one each
  * Products run in bf16 with fp32 accumulation, the softmax in fp32, its
- * weights rounded to bf16 for the second product; the output is rounded once.  Two calls on the same plan and inputs give the same
- * bits.
+ * weights rounded to bf16 for the second product; the output is rounded once.
+ * Two calls on the same plan and inputs give the same bits.
  */
 int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan,
                      const mla_head_rows* q_nope, const mla_head_rows* q_rope,

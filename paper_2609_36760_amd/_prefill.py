@@ -114,12 +114,12 @@ def _on_device(*tensors) -> None:
 
 def _rows(t, n: int, width: int, what: str) -> None:
     """``t``: bf16 [n, width] with unit stride in the last axis."""
-    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or t.stride(1) != 1 or t.dtype not in BF16:
+    if t.shape != (n, width) or t.stride(1) != 1 or t.dtype not in BF16:
         raise ValueError(f"{what}: bf16 [{n}, {width}] rows with unit stride, got {tuple(t.shape)} strides {t.stride()}")
 
 
 def _ints(t, n: int, dtype, what: str) -> None:
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous {dtype} [{n}], got {tuple(t.shape)}, {t.dtype}")
 
 
@@ -261,9 +261,10 @@ def mla_plan_prefill(q_lens, kv_lens, H: int, causal: bool = True, q_starts=None
 
 
 def _heads(t, rows: int, H: int, width: int, what: str) -> mla_head_rows:
-    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != H or t.shape[2] != width or t.stride(2) != 1 or t.dtype not in BF16:
-        raise ValueError(f"{what}: bf16 [>= {rows}, {H}, {width}] rows with unit stride, got {tuple(t.shape)} strides {t.stride()}")
-    return mla_head_rows(t.data_ptr(), t.stride(0), t.stride(1))
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < rows or shape[1:] != (H, width) or strides[2] != 1 or t.dtype not in BF16:
+        raise ValueError(f"{what}: bf16 [>= {rows}, {H}, {width}] rows with unit stride, got {tuple(shape)} strides {strides}")
+    return mla_head_rows(t.data_ptr(), strides[0], strides[1])
 
 
 def mla_prefill_attn(info, plan, q_nope, q_rope, k_nope, k_rope, v, softmax_scale, out, lse=None, workspace=None,
@@ -273,10 +274,11 @@ def mla_prefill_attn(info, plan, q_nope, q_rope, k_nope, k_rope, v, softmax_scal
     and [keys, 64], values [keys, H, 128] into ``out`` [rows, H, 128] and
     ``lse`` fp32 [rows, H].  ``workspace``: at least ``info.workspace_bytes``."""
     T, K, H = info.total_q, info.total_kv, info.H
-    if k_rope.dim() != 2 or k_rope.shape[0] < K or k_rope.shape[1] != D_R or k_rope.stride(1) != 1 or k_rope.dtype not in BF16:
-        raise ValueError(f"k_rope: bf16 [>= {K}, 64] rows with unit stride, got {tuple(k_rope.shape)}")
+    shape, strides = k_rope.shape, k_rope.stride()
+    if len(shape) != 2 or shape[0] < K or shape[1] != D_R or strides[1] != 1 or k_rope.dtype not in BF16:
+        raise ValueError(f"k_rope: bf16 [>= {K}, 64] rows with unit stride, got {tuple(shape)}")
     rows = (_heads(q_nope, T, H, D_NOPE, "q_nope"), _heads(q_rope, T, H, D_R, "q_rope"),
-            _heads(k_nope, K, H, D_NOPE, "k_nope"), mla_head_rows(k_rope.data_ptr(), k_rope.stride(0), 0),
+            _heads(k_nope, K, H, D_NOPE, "k_nope"), mla_head_rows(k_rope.data_ptr(), strides[0], 0),
             _heads(v, K, H, D_V, "v"))
     o = _heads(out, T, H, D_V, "out")
     _ints(plan, info.plan_ints, I32, "plan")
@@ -286,5 +288,5 @@ def mla_prefill_attn(info, plan, q_nope, q_rope, k_nope, k_rope, v, softmax_scal
     _on_device(plan, q_nope, q_rope, k_nope, k_rope, v, out, lse, workspace)
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     mb._check("mla_prefill_attn", library().mla_prefill_attn(
-        ctypes.byref(info), plan.data_ptr(), *(ctypes.byref(r) for r in rows), float(softmax_scale), o.data,
+        ctypes.byref(info), plan.data_ptr(), *map(ctypes.byref, rows), float(softmax_scale), o.data,
         o.stride_t, o.stride_h, mb._ptr(lse), mb._ptr(workspace), size, mb._stream(stream)))

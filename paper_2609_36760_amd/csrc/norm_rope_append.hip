@@ -7,6 +7,10 @@
 // 16 bytes a lane), or the RoPE keys of 8 tokens (8 lanes each).  The content
 // waves come first; the RoPE waves run beside them.
 //
+// Memory bounds it where there are many tokens: 1152 bytes read, as many written dense
+// and 324 (4 bits) packed.  8 x 8K tokens, protected, and their gather: 83 us, caches
+// cold, of 58 at a copy's rate.
+//
 // The norm: squares of bf16 values are exact in fp64, and the sum of 512 of
 // them is rounded so far below bf16 that the order of the reduction does not
 // show; x w is exact there too, and its product with 1 / sqrt(mean + eps) is

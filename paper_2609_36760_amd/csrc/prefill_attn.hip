@@ -2,9 +2,8 @@
 // q_rope . k_rope)) v over 192 score channels (64 of them one key row for all
 // heads) and 128 value channels, for blocks of query rows.
 //
-// One workgroup takes a plan's work item for one head: G groups of 32 query rows
-// per wave, all waves over the same key tiles.  Per tile of KT keys (KT / 32 key
-// blocks):
+// One workgroup takes blocks of query rows of one head: G groups of 32 rows per
+// wave, all waves over the same key tiles.  Per tile of KT keys (KT / 32 key blocks):
 //   1. the tile's rows go from memory straight into LDS, two tiles ahead, 16
 //      bytes a lane; LDS places are linear in the lane, so the bank swizzle is
 //      applied to which 16 bytes of a row a lane fetches;
@@ -13,19 +12,31 @@
 //      ends up with one row's scores for half of the keys, its partner lane ^ 32
 //      with the other half;
 //   3. one pass over the scores: weights 2^(s - reference) in fp32 on the row's
-//      running reference, rounded to bf16, their sums;
+//      reference, rounded to bf16, their sums;
 //   4. O^T[channel][row] += V^T . P^T (M = 128 channels in 4 blocks, K = KT
 //      keys): P^T comes straight from the score registers, because the
 //      transposing LDS reads fetch V's keys in the order in which the score
 //      product left them.
 //
-// What bounds it is the matrix unit, and the power that everything around it
-// draws (the clock falls from 2.4 to 1.65 GHz under the two-waves-per-SIMD form
-// of this kernel).  So a wave has two row groups where there are rows enough:
-// every operand read from LDS feeds two products, every tile staged 256 rows.
-// Such a wave has a SIMD to itself (acc 128, Q 96, scores 64, weights 32
-// registers), and overlaps by its own instruction order: the softmax of one key
-// block runs between the products of the next.
+// Two shapes (which one: choose_rows in mla_prefill_abi.cpp):
+//   256 rows, 64 keys: a wave has two row groups and a SIMD to itself (acc 128,
+//     Q 96, scores 64, weights 32 registers): every operand read from LDS feeds two
+//     products, every tile staged 256 rows, and the softmax of one key block runs
+//     between the products of the next, by the order of the instructions.  (The form
+//     with two 32-row waves per SIMD reads twice as much LDS and memory per product;
+//     the power that it drew brought the clock from 2.4 to 1.65 GHz, 8K keys, 128
+//     heads, causal: 3.16 ms.)  A workgroup has a CU to itself, so nothing would hide a
+//     block's beginning and end: it goes through a list of blocks, and the first two
+//     tiles and the queries of the next come in while the last tile is worked on.
+//   128 rows, 32 keys: two workgroups per CU overlap each other; for up to 128 rows
+//     per sequence, where the reads of keys and values are the bound.
+//
+// Measured (MI355X), 256 rows: 8K keys, causal, 128 heads 2.21 ms, 1240 TFLOP/s of
+// the visible keys' products; 8K x 8K, 64 heads 2.02-2.12 ms, 1300-1360 (all-zero
+// inputs 1.51 ms, 1820: what is left is the power limit, 1.75 GHz).  A tile takes 3.5K
+// cycles for 2.56K of products, a block 13K beside its tiles.  128 rows: one token on
+// 32 x 2K keys, 32 heads 189 us, 5.7 TB/s; 256 prompts of 64, 64 heads 250 us (245 at a
+// copy's rate).
 //
 // Roundings: the weights are bf16 operands of the second product (at most 2^-8
 // of a weight, as the bf16 output's own rounding; bf16 values allow no wider
@@ -36,14 +47,15 @@
 // four more vector instructions a pair.)
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
-// any reference that keeps them from overflow: a row's is its maximum over its
-// first 32 keys, and it stays, and no later tile is searched for maxima, as long
-// as a block's weights add up to less than 2^100 -- scores 69 above the first
-// ones in natural units.  A workgroup that meets larger sums, sums that are no
-// number, or values that are not finite where a row is hidden from them, does its
-// rows over in careful_rows, which moves references tile by tile.  (Kept apart, so
-// that the accumulators have one place throughout: any other use of them between
-// the products made the compiler copy them in every tile.)
+// any reference near their scores: a row's is its largest score of the first 32
+// keys that its wave meets, seen by the row or not, and it stays; no later tile is
+// searched for maxima.  A row whose weights add up to less than 2^-60 or more than
+// 2^60 (scores 41 off in natural units; values up to 2^67 stay finite in the sums),
+// or to no number, or that is hidden from values that are not finite, sends its
+// workgroup through careful_rows, which does the block over and moves references
+// tile by tile.  (Kept apart, so that the accumulators have one place throughout:
+// any other use of them between the products made the compiler copy them in every
+// tile.)
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
