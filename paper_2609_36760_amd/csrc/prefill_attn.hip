@@ -851,17 +851,35 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
     const int part0 = max(g.part0, 0), parts = min(g.num_parts, a.num_parts - part0);
     const int64_t step = static_cast<int64_t>(a.H) * a.part_rows;
     const int64_t row = part0 * step + static_cast<int64_t>(head) * a.part_rows + r;
-    float top = kUnset;
-    for (int j = 0; j < parts; ++j) top = fmaxf(top, a.part_m[row + j * step]);
-    float sum = 0.0f;
+    // the loads of eight partials before any is used (a token on 64K keys, 16 heads, 32
+    // splits: a call of 114 us with one after the other, 111 so)
+    float top = kUnset, sum = 0.0f;
     float2 o = make_float2(0.0f, 0.0f);
-    for (int j = 0; j < parts; ++j) {
-        const int64_t at = row + j * step;
-        const float f = exp2f(a.part_m[at] - top) * a.part_l[at];
-        const float2 x = *reinterpret_cast<const float2*>(a.part_o + at * kValue + 2 * lane);
-        sum += f;
-        o.x = fmaf(f, x.x, o.x);
-        o.y = fmaf(f, x.y, o.y);
+    for (int j0 = 0; j0 < parts; j0 += 8) {
+        float m[8], l[8];
+        float2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t at = row + min(j0 + i, parts - 1) * step;
+            m[i] = a.part_m[at];
+            l[i] = a.part_l[at];
+            x[i] = *reinterpret_cast<const float2*>(a.part_o + at * kValue + 2 * lane);
+        }
+        const float before = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, m[i]);
+        const float kept = exp2f(before - top);
+        sum *= kept;
+        o.x *= kept;
+        o.y *= kept;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (j0 + i >= parts) break;
+            const float f = exp2f(m[i] - top) * l[i];
+            sum += f;
+            o.x = fmaf(f, x[i].x, o.x);
+            o.y = fmaf(f, x[i].y, o.y);
+        }
     }
     const bool none = min(static_cast<int64_t>(g.kv_len), static_cast<int64_t>(g.seen0) + r) <= 0;
     const float inv = none ? 0.0f : 1.0f / sum;
