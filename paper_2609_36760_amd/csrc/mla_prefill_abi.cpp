@@ -214,7 +214,9 @@ int64_t plan_ints(const mla_prefill_plan& p) {
 // end.  Blocks that begin together go through their keys from the first on; where
 // the lists are spread out, the longest block begins first and all end together,
 // so they go from the last key down: either way they read the same keys at the
-// same time.  `items` in the order of the plan.
+// same time (8K keys, 128 heads: 2271 us against 2311 all upwards; where a head's keys
+// fit the L2 it costs, 4 of 4K, 64 heads: 1305 against 1276).  `items` in the order of
+// the plan.
 constexpr int32_t kItemTiles = 5;       // an item's fixed cost, in tiles
 constexpr int32_t kLastRounds = 2;
 constexpr int32_t kL2Tiles = 96;        // tiles of a head that fill an XCD's L2 (40 KiB each)

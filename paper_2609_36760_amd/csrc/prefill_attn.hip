@@ -98,10 +98,16 @@ __device__ __forceinline__ void scores_past(f32x16& c) { asm volatile("s_nop 4" 
 // base goes through a scalar instruction here: if the compiler brings it back by
 // v_readlane, a memory instruction may not read it for five wait states, and it does
 // not see that one does.  (It is the wait state after the write of M0 as well; five
-// of s_nop in its place took 1 % more of a prompt's time.)
+// of s_nop in its place took 1 % more of a prompt's time.)  kOnce: rows that one block
+// reads, past the caches; those that several blocks read stay (12 ragged prompts, 128
+// heads: 774 us against 839; 4 of 4K, 64 heads: 1272 against 1414).
+template <bool kOnce>
 __device__ __forceinline__ void dma16(const uint8_t* base, uint32_t voff, uint32_t lds) {
     uint64_t from;
-    asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0 nt" : "=&s"(from) : "v"(voff), "s"(base), "{m0}"(lds) : "memory");
+    if constexpr (kOnce)
+        asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0 nt" : "=&s"(from) : "v"(voff), "s"(base), "{m0}"(lds) : "memory");
+    else
+        asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(from) : "v"(voff), "s"(base), "{m0}"(lds) : "memory");
 }
 
 // Maximum / sum of a value and its copy in lane ^ 32.
@@ -238,9 +244,9 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
             const uint32_t row = static_cast<uint32_t>(min(x, last));
             const uint32_t c = static_cast<uint32_t>((l & 7) ^ (plane < 3 ? score_xor(x) : value_xor(x))) * 16;
             const uint32_t at = lds0 + to + plane * S::plane + block * 1024;
-            if (plane < 2) dma16(n + plane * kRow, row * kn_b + c, at);
-            else if (plane == 2) dma16(r, row * kr_b + c, at);
-            else dma16(v + (plane - 3) * kRow, row * vv_b + c, at);
+            if (plane < 2) dma16<!S::listed>(n + plane * kRow, row * kn_b + c, at);
+            else if (plane == 2) dma16<!S::listed>(r, row * kr_b + c, at);
+            else dma16<!S::listed>(v + (plane - 3) * kRow, row * vv_b + c, at);
         }
     };
     // Load i of a tile that is there whole: a wave's loads are a swizzle period (16
@@ -253,9 +259,9 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     auto load_whole = [&](int i, uint32_t to, const uint8_t* n, const uint8_t* r, const uint8_t* v) __attribute__((always_inline)) {
         const int plane = i * NW / S::blocks, first = i * NW % S::blocks;
         const uint32_t at = lds0 + to + plane * S::plane + (first + wave) * 1024;
-        if (plane < 2) dma16(n + plane * kRow + static_cast<uint64_t>(first * 8) * kn_b, at_n[first & 1], at);
-        else if (plane == 2) dma16(r + static_cast<uint64_t>(first * 8) * kr_b, at_r[first & 1], at);
-        else dma16(v + (plane - 3) * kRow + static_cast<uint64_t>(first * 8) * vv_b, at_v, at);
+        if (plane < 2) dma16<!S::listed>(n + plane * kRow + static_cast<uint64_t>(first * 8) * kn_b, at_n[first & 1], at);
+        else if (plane == 2) dma16<!S::listed>(r + static_cast<uint64_t>(first * 8) * kr_b, at_r[first & 1], at);
+        else dma16<!S::listed>(v + (plane - 3) * kRow + static_cast<uint64_t>(first * 8) * vv_b, at_v, at);
     };
     // A value that some row does not see must not reach that row through 0 * inf or
     // 0 * NaN.  A wave looks through the values that it staged itself, once they are
