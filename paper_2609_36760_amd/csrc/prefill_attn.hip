@@ -584,7 +584,6 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
 #pragma unroll
                 for (int j = 0; j < 2; ++j) vt[j] = at_tile(va[j], next);
             } else {
-                if (more && t + 1 == cur.tiles) load_queries(following);    // (no score product of this block is left)
                 value_phase(0, values_of(1), [&](int slot) __attribute__((always_inline)) { early(1, slot, kPart); });
                 weigh_rest(1, kEarly, kPart);
                 value_phase(1, keep, nothing);
@@ -715,14 +714,12 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
             ++t;
             off = after(off);
         }
-        // A wave that is done early loads its queries after the last tile's meeting, where
-        // no other wave waits for them.
-        const bool early_end = t_end < cur.tiles || some == 0;
         for (; t < cur.tiles; ++t, off = after(off)) {
             meet(t, off);
             stage_ahead(t, off);
         }
-        if (more && early_end) load_queries(following);
+        // (after the last tile's meeting, where no other wave waits for them)
+        if (more) load_queries(following);
         // Whether any wave wants the rows done over.
 #pragma unroll
         for (int g = 0; g < G; ++g) {
