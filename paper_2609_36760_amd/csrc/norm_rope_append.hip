@@ -121,10 +121,11 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(NormRopeArgs
                 const double r = lane_value(inv, i * (64 / kTok));
                 float x[8];
                 wc::widen_bf16x8(raw[i], x);
-                uint32_t y[8];
+                uint32_t y[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = rt::bf16_of(static_cast<double>(x[j]) * w[j] * r);
-                raw[i] = make_uint4(y[0] | y[1] << 16, y[2] | y[3] << 16, y[4] | y[5] << 16, y[6] | y[7] << 16);
+                for (int j = 0; j < 4; ++j)
+                    y[j] = rt::bf16x2_of(static_cast<double>(x[2 * j]) * w[2 * j] * r, static_cast<double>(x[2 * j + 1]) * w[2 * j + 1] * r);
+                raw[i] = make_uint4(y[0], y[1], y[2], y[3]);
             }
         }
 #pragma unroll

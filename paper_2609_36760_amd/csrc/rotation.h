@@ -17,9 +17,14 @@
 namespace mla {
 namespace rt {
 
-__device__ __forceinline__ uint32_t bf16_of(double v) {
-    const __bf16 b = static_cast<__bf16>(static_cast<float>(v));
-    return __builtin_bit_cast(uint16_t, b);
+// Two values rounded to fp32, then to bf16.  (Kept apart by the empty asm: as one
+// conversion from fp64 to bf16 the compiler makes eight instructions of it.)
+__device__ __forceinline__ uint32_t bf16x2_of(double lo, double hi) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    float a = static_cast<float>(lo), b = static_cast<float>(hi);
+    asm("" : "+v"(a), "+v"(b));
+    const bf16x2 v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 // Row of `table` for a device-resident position, kept inside it.
@@ -70,13 +75,13 @@ __device__ __forceinline__ uint4 rotate(const uint4 raw, const Angles& a, bool h
         for (int i = 0; i < 4; ++i) {
             const double lo = static_cast<double>(x[2 * i]) * a.c[2 * i] + sign * y[2 * i] * a.s[2 * i];
             const double hi = static_cast<double>(x[2 * i + 1]) * a.c[2 * i + 1] + sign * y[2 * i + 1] * a.s[2 * i + 1];
-            w[i] = bf16_of(lo) | (bf16_of(hi) << 16);
+            w[i] = bf16x2_of(lo, hi);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const double p = x[2 * i], q = x[2 * i + 1], c = a.c[i], s = a.s[i];
-            w[i] = bf16_of(p * c - q * s) | (bf16_of(p * s + q * c) << 16);
+            w[i] = bf16x2_of(p * c - q * s, p * s + q * c);
         }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
