@@ -26,15 +26,17 @@
 //     with two 32-row waves per SIMD reads twice as much LDS and memory per product;
 //     the power that it drew brought the clock from 2.4 to 1.65 GHz, 8K keys, 128
 //     heads, causal: 3.16 ms.)  A workgroup has a CU to itself, so nothing would hide a
-//     block's beginning and end: it goes through a list of blocks, and the first two
-//     tiles and the queries of the next come in while the last tile is worked on.
+//     block's beginning and end: it goes through a list of blocks; the first two tiles
+//     of the next come in while the last ones are worked on, its queries while the
+//     results go out (loaded earlier, they kept other waves waiting: 12 ragged prompts,
+//     128 heads 842 us against 819, then 769 against 750).
 //   128 rows, 32 keys: two workgroups per CU overlap each other; for up to 128 rows
 //     per sequence, where the reads of keys and values are the bound.
 //
-// Measured (MI355X), 256 rows: 8K keys, causal, 128 heads 2.21 ms, 1240 TFLOP/s of
+// Measured (MI355X), 256 rows: 8K keys, causal, 128 heads 2.24-2.31 ms, 1190-1230 TFLOP/s of
 // the visible keys' products; 8K x 8K, 64 heads 2.02-2.12 ms, 1300-1360 (all-zero
 // inputs 1.51 ms, 1820: what is left is the power limit, 1.75 GHz).  A tile takes 3.5K
-// cycles for 2.56K of products, a block 13K beside its tiles.  128 rows: one token on
+// cycles for 2.56K of products, a block about 12K beside its tiles.  128 rows: one token on
 // 32 x 2K keys, 32 heads 189 us, 5.7 TB/s; 256 prompts of 64, 64 heads 250 us (245 at a
 // copy's rate).
 //
