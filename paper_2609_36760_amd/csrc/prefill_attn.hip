@@ -612,7 +612,9 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                 for (int i = 0; i < 16; i += 4)
                     *reinterpret_cast<float4*>(to + 32 * m + 2 * i) = make_float4(o[m][i] * inv, o[m][i + 1] * inv, o[m][i + 2] * inv, o[m][i + 3] * inv);
             if (half == 0) {
-                a.part_m[row] = ref;
+                // a partial that weighs nothing has no reference: a row that sees no key of
+                // the split may have taken its own from keys that it does not see
+                a.part_m[row] = total == 0.0f ? kUnset : ref;
                 a.part_l[row] = total;
             }
             return;
