@@ -211,6 +211,11 @@ typedef struct mla_head_rows {
  *              info->workspace_bytes); calls that may overlap need one each
  * Products run in bf16 with fp32 accumulation, the softmax in fp32, its
  * weights rounded to bf16 for the second product; the output is rounded once.
+ * Finite inputs whose scores are finite and whose values are at most 2^126 in size
+ * give finite outputs; weights under 2^-66 of a row's sum, and products of weight
+ * and value under 2^-66, may be taken as 0.  A row that sees a value that is not
+ * finite is not finite in that channel (NaN in an infinity's place, where its
+ * weight is taken as 0).
  * Two calls on the same plan and inputs give the same bits.
  */
 int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan,

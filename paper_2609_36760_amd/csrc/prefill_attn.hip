@@ -49,15 +49,20 @@
 // four more vector instructions a pair.)
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
-// any reference near their scores: a row's is its largest score of the first 32
-// keys that its wave meets, seen by the row or not, and it stays; no later tile is
-// searched for maxima.  A row whose weights add up to less than 2^-60 or more than
-// 2^60 (scores 41 off in natural units; values up to 2^67 stay finite in the sums),
+// any reference near their scores: a row's lies 40 log2 units above its largest
+// score of the first 32 keys that its wave meets, seen by the row or not, but at most
+// 58 above that of the first of them if it sees that one, and it stays; no later tile
+// is searched for maxima.  The 40 units keep the usual sums small: weights that add up
+// to less than 2^-2 bring no finite value (below 2^128) out of fp32's range.  A row
+// whose weights add up to less than 2^-60 or more than 2^-2 (it sees none of those 32
+// keys and scores 14 natural units below them, or 26 above them, less for many keys),
 // or to no number, or that is hidden from values that are not finite, sends its
-// workgroup through careful_rows, which does the block over and moves references
-// tile by tile.  (Kept apart, so that the accumulators have one place throughout:
-// any other use of them between the products made the compiler copy them in every
-// tile.)
+// workgroup through careful_rows, which does the block over and moves references tile
+// by tile, 32 units above the largest score so far (2^30 keys of equal weight add up
+// to 2^-2).  Weights under 2^-66 of a row's sum, and products
+// with a value under 2^-66, may leave fp32's range below.  (Kept apart, so that the
+// accumulators have one place throughout: any other use of them between the products
+// made the compiler copy them in every tile.)
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -78,7 +83,10 @@ using kc::lds_i16x4;
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;
+constexpr float kLeast = 0x1p-60f, kMost = 0x1p-2f;     // sums that stand
+constexpr float kAbove = 40.0f, kAboveMoved = 32.0f;    // of a fixed / a moved reference, above the scores it is taken from
+constexpr float kAboveFirst = 58.0f;                    // at most above a seen score
+constexpr float kMergeScale = 0x1p-32f;                 // of a merge's weights: any number of finite rows stays finite
 constexpr float kUnset = -FLT_MAX;
 
 // Score products accumulate in vector registers, with the queries in accumulation
@@ -389,12 +397,18 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     f32x16 s[KB][G];
     uint32_t w[G][8 * KB];                  // weights, bf16 pairs
     float block_sum[G];
-    // the row's largest score of block b, log2 units
-    auto top_of = [&](int b, int g) __attribute__((always_inline)) {
-        float top = s[b][g][0];
+    int here[G];                            // keys of the tile that the lane's rows see, less 4 half
+    // the row's largest score of the tile's first key block, log2 units
+    auto top_of = [&](int g) __attribute__((always_inline)) {
+        float top = s[0][g][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][g][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][g][i]);
         return max_halves(top) * c2;
+    };
+    // the row's score of its first key
+    auto first_of = [&](int g) __attribute__((always_inline)) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[0][g][0]), __float_as_uint(s[0][g][0]), false, false);
+        return __uint_as_float(r[0]) * c2;
     };
     auto weights = [&](int g, int ks) __attribute__((always_inline)) {
         const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
@@ -464,7 +478,6 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     // early units start in slot 4 of the value phase (4 products after the scores), the
     // late ones, and the test of the sums, fill the score phase.
     float argument, weight, kept;               // in the units' pipeline
-    int here[G];                                // keys of the tile that the lane's rows see, less 4 half
     auto set_here = [&](int key) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < G; ++g) here[g] = sees_of(cur, r0 + 32 * g + col) - key - 4 * half;
@@ -526,7 +539,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         for (int g = 0; g < G; ++g) scores_ready(s[0][g]);
         if (first) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, top_of(0, g));
+            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, fminf(top_of(g) + kAbove, here[g] + 4 * half > 0 ? first_of(g) + kAboveFirst : INFINITY));
         }
 #pragma unroll
         for (int u = 0; u < kEarly; ++u) unit(0, u, true);
@@ -613,9 +626,10 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                     *reinterpret_cast<float4*>(to + 32 * m + 2 * i) = make_float4(o[m][i] * inv, o[m][i + 1] * inv, o[m][i + 2] * inv, o[m][i + 3] * inv);
             if (half == 0) {
                 // a partial that weighs nothing has no reference: a row that sees no key of
-                // the split may have taken its own from keys that it does not see
-                a.part_m[row] = total == 0.0f ? kUnset : ref;
-                a.part_l[row] = total;
+                // the split may have taken its own from keys that it does not see.  Others
+                // are kept as 2^m l with l in [0.5, 1): the largest m is then the merge's.
+                a.part_m[row] = total == 0.0f ? kUnset : ref + static_cast<float>(__builtin_amdgcn_frexp_expf(total));
+                a.part_l[row] = __builtin_amdgcn_frexp_mantf(total);
             }
             return;
         }
@@ -784,7 +798,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                             z[i] = (i & 3) + 8 * (i >> 2) < seen_here ? z[i] : -INFINITY;
                             top = fmaxf(top, z[i]);
                         }
-                        const float to = fminf(fmaxf(rc, max_halves(top) * c2), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
+                        const float to = fminf(fmaxf(rc, max_halves(top) * c2 + kAboveMoved), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
                         const float f = __builtin_amdgcn_exp2f(rc - to);
                         rc = to;
                         sc *= f;
@@ -882,7 +896,7 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (j0 + i >= parts) break;
-            const float f = exp2f(m[i] - top) * l[i];
+            const float f = exp2f(m[i] - top) * (l[i] * kMergeScale);
             sum += f;
             o.x = fmaf(f, x[i].x, o.x);
             o.y = fmaf(f, x[i].y, o.y);
@@ -894,7 +908,7 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
     *reinterpret_cast<uint32_t*>(a.out + q * a.out_stride_t + static_cast<int64_t>(head) * a.out_stride_h + 2 * lane) =
         kc::pack_bf16x2(o.x * inv, o.y * inv);
     if (a.lse != nullptr && lane == 0)
-        a.lse[q * a.H + head] = none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        a.lse[q * a.H + head] = none ? -INFINITY : (top + log2f(sum / kMergeScale)) * 0.6931471805599453f;
 }
 
 }  // namespace

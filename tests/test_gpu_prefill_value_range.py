@@ -1,0 +1,48 @@
+"""Expanded attention on very large and very small values (GPU): finite inputs
+give finite outputs, whatever weights the values meet on the way -- scores that
+grow by tens of units behind a row's first keys, many keys of equal weight,
+blocks done over, and partials that are merged.
+"""
+import pytest
+
+from unseen_keys import check_finite_case
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [([200], [1500]), ([90], [700]), ([1], [64]), ([3], [5000]), ([257], [3000]), ([1, 2, 1], [3000, 70, 4099])]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("grow", [0.0, 10.0, 31.0, 60.0, 200.0, -35.0, -80.0])
+@pytest.mark.parametrize("top", [2.0 ** 126, 2.0 ** 84, 2.0 ** -40])
+@pytest.mark.parametrize("q,kv", SHAPES)
+def test_values_far_from_one(q, kv, causal, grow, top):
+    import torch
+
+    from test_gpu_prefill import TAU, Call
+    c = Call(q, kv, 2, causal, seed=21)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(22)
+    # head 0: values of either sign; head 1: of one sign, so that nothing cancels
+    c.v[:] = ((torch.rand(c.v.shape, generator=g, device="cuda") * 1.98 - 0.99) * top).bfloat16()
+    c.v[:, 1] = c.v[:, 1].abs()
+    # all keys but the first 40 of each sequence stand `grow` above those (40: a tile's edge is at 32 and 64)
+    c.q_nope[:, :, 0] = 32.0
+    c.k_nope[:, :, 0] = grow / (TAU * 32.0)
+    for e in c.k0:
+        c.k_nope[e:e + 40, :, 0] = 0.0
+    c.run()
+    check_finite_case(c, range(2), f"{q} on {kv}, values to {top:.3g}, grown by {grow}")
+
+
+@pytest.mark.parametrize("q,kv", [([128], [770]), ([250], [1537])])
+@pytest.mark.parametrize("top", [2.0 ** 126, 2.0 ** -40])
+def test_values_far_from_one_under_equal_weights(q, kv, top):
+    """All scores 0: a row's sum is its number of keys."""
+    from test_gpu_prefill import Call
+    c = Call(q, kv, 2, True, seed=23)
+    c.q_nope[:], c.q_rope[:] = 0.0, 0.0
+    c.v[:, 0] = top
+    c.v[:, 1] = -top
+    c.run()
+    check_finite_case(c, range(2), f"{q} on {kv}, all values {top:.3g}")
