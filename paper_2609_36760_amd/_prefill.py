@@ -285,6 +285,7 @@ def mla_prefill_attn(info, plan, q_nope, q_rope, k_nope, k_rope, v, softmax_scal
     if lse is not None and (lse.dim() != 2 or lse.shape[0] < T or lse.shape[1] != H or not lse.is_contiguous() or
                             lse.dtype != F32):
         raise ValueError(f"lse: contiguous fp32 [>= {T}, {H}], got {tuple(lse.shape)}")
+    _need(workspace is None or workspace.is_contiguous(), "workspace: contiguous")
     _on_device(plan, q_nope, q_rope, k_nope, k_rope, v, out, lse, workspace)
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     mb._check("mla_prefill_attn", library().mla_prefill_attn(
