@@ -243,11 +243,19 @@ def mla_lowbit_gather_protected(fmt, policy, cache, num_pages, block_table, cu_r
         prot_slot.data_ptr(), *o, mb._stream(stream)))
 
 
+def _int32s(x) -> np.ndarray:
+    a = np.atleast_1d(np.asarray(x))
+    with np.errstate(invalid="ignore"):
+        b = np.ascontiguousarray(a, dtype=np.int32)
+    _need(np.array_equal(a, b), "lengths and starts: whole numbers of 32 bits")
+    return b
+
+
 def mla_plan_prefill(q_lens, kv_lens, H: int, causal: bool = True, q_starts=None, kv_starts=None):
     """Host planner of the expanded attention: ``(plan int32, info)``.  The
     caller keeps a device copy of ``plan``; it serves every call with these
     lengths."""
-    lens = [None if x is None else np.ascontiguousarray(x, dtype=np.int32) for x in (q_lens, kv_lens, q_starts, kv_starts)]
+    lens = [None if x is None else _int32s(x) for x in (q_lens, kv_lens, q_starts, kv_starts)]
     B = lens[0].size
     for x in lens:
         _need(x is None or (x.ndim == 1 and x.size == B), "lengths and starts: one per sequence")
