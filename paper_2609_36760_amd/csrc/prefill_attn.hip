@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         x.kv_row = min(max(ip->kv_row, 0), a.total_kv);
         x.key1 = min(max(ip->key1, 0), a.total_kv - x.kv_row);
         x.key0 = min(max(ip->key0, 0), x.key1);
-        x.seen0 = ip->seen0;
+        x.seen0 = max(ip->seen0, -S::rows);      // (no row sees a key: differences from it stay within 32 bits)
         x.part = min(ip->part, a.num_parts - 1);
         x.tiles = (x.key1 - x.key0 + KT - 1) / KT;
         x.down = down;
