@@ -868,7 +868,7 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
     if (id >= static_cast<uint32_t>(a.num_merges)) return;
     const int head = static_cast<int>(rest / a.part_rows), r = static_cast<int>(rest % a.part_rows);
     const PrefillMerge g = a.merges[id];
-    if (r >= g.q_rows || g.q_row < 0 || g.q_row + r >= a.total_q) return;
+    if (r >= g.q_rows || g.q_row < 0 || g.q_row >= a.total_q - r) return;
     const int part0 = max(g.part0, 0), parts = min(g.num_parts, a.num_parts - part0);
     const int64_t step = static_cast<int64_t>(a.H) * a.part_rows;
     const int64_t row = part0 * step + static_cast<int64_t>(head) * a.part_rows + r;
