@@ -505,7 +505,9 @@ int mla_prefill_attn(const mla_prefill_plan* info, const int32_t* plan, const ml
     if (info == nullptr || info->B < 0 || info->H <= 0) return MLA_EINVAL;
     if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.0f)) return MLA_EINVAL;
     // what the planner fills: nothing else is launched
+    // (no more merges or partials than items, so that the products below stay within 64 bits)
     if (info->num_items < 0 || info->num_merges < 0 || info->num_parts < 0 || info->total_q < 0 ||
+        info->num_merges > info->num_items || info->num_parts > info->num_items ||
         info->total_kv < 0 || info->total_q > kMaxLen || info->total_kv > kMaxLen)
         return MLA_EINVAL;
     if (info->plan_ints != plan_ints(*info)) return MLA_EINVAL;

@@ -220,6 +220,11 @@ void infos() {
         p.plan_ints = v;
         CHECK(attend(p, plan) == MLA_EINVAL);
     }
+    // more partials than items is no planner's
+    mla_prefill_plan p = good;
+    p.num_parts = p.num_items + 1;
+    p.workspace_bytes = static_cast<int64_t>(p.num_parts) * p.H * p.part_rows * mla::kPartRowBytes;
+    CHECK(attend(p, plan) == MLA_EINVAL);
 }
 
 void others() {
