@@ -539,7 +539,10 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         for (int g = 0; g < G; ++g) scores_ready(s[0][g]);
         if (first) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, fminf(top_of(g) + kAbove, here[g] + 4 * half > 0 ? first_of(g) + kAboveFirst : INFINITY));
+            for (int g = 0; g < G; ++g) {
+                const float one = first_of(g);      // (a key that scores -inf weighs nothing)
+                ref[g] = fmaxf(kUnset, fminf(top_of(g) + kAbove, here[g] + 4 * half > 0 && one >= kUnset ? one + kAboveFirst : INFINITY));
+            }
         }
 #pragma unroll
         for (int u = 0; u < kEarly; ++u) unit(0, u, true);

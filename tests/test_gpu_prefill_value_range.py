@@ -46,3 +46,34 @@ def test_values_far_from_one_under_equal_weights(q, kv, top):
     c.v[:, 1] = -top
     c.run()
     check_finite_case(c, range(2), f"{q} on {kv}, all values {top:.3g}")
+
+
+@pytest.mark.parametrize("q,kv,causal", [([200], [1500], True), ([90], [700], True), ([1], [64], True), ([128], [770], True),
+                                         ([256], [8200], True), ([70, 3], [70, 5000], False)])
+@pytest.mark.parametrize("which", ["first", "every third", "last", "first 100"])
+def test_seen_keys_that_score_minus_infinity(q, kv, causal, which):
+    """They weigh nothing, and what the others give is exact to the usual roundings."""
+    from test_gpu_prefill import Call
+    c = Call(q, kv, 2, causal, seed=24)
+    c.q_nope[:, :, 0] = c.q_nope[:, :, 0].abs() + 0.5
+    for e, nk in zip(c.k0, kv):
+        k = c.k_nope[e:e + nk, :, 0]
+        at = {"first": slice(0, 1), "every third": slice(0, nk, 3), "last": slice(nk - 1, nk), "first 100": slice(0, min(100, nk - 1))}[which]
+        k[at] = -float("inf")
+    c.run()
+    check_some_rows(c, f"{q} on {kv}, {which} at -inf")
+
+
+def check_some_rows(c, what):
+    """check_finite_case without the causal rows whose keys all score -inf (their output is not a number)."""
+    import torch
+    torch.cuda.synchronize()
+    for b, (nq, nk) in enumerate(zip(c.q_lens, c.kv_lens)):
+        a, e = c.q0[b], c.k0[b]
+        finite = torch.isfinite(c.k_nope[e:e + nk, 0, 0])
+        for i in range(nq):
+            sees = nk - nq + i + 1 if c.causal else nk
+            if sees > 0 and not finite[:sees].any():
+                assert bool(c.out[a + i].isnan().all()) and bool((c.lse[a + i] == -float("inf")).all())
+                c.out[a + i] = 0.0
+    check_finite_case(c, range(2), what)
