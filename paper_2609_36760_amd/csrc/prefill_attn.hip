@@ -49,20 +49,20 @@
 // four more vector instructions a pair.)
 //
 // The reference.  bf16 has the range of fp32, so a row's weights may be taken on
-// any reference near their scores: a row's lies 40 log2 units above its largest
-// score of the first 32 keys that its wave meets, seen by the row or not, but at most
-// 58 above that of the first of them if it sees that one, and it stays; no later tile
-// is searched for maxima.  The 40 units keep the usual sums small: weights that add up
-// to less than 2^-2 bring no finite value (below 2^128) out of fp32's range.  A row
-// whose weights add up to less than 2^-60 or more than 2^-2 (it sees none of those 32
-// keys and scores 14 natural units below them, or 26 above them, less for many keys),
-// or to no number, or that is hidden from values that are not finite, sends its
-// workgroup through careful_rows, which does the block over and moves references tile
-// by tile, 32 units above the largest score so far (2^30 keys of equal weight add up
-// to 2^-2).  Weights under 2^-66 of a row's sum, and products
-// with a value under 2^-66, may leave fp32's range below.  (Kept apart, so that the
-// accumulators have one place throughout: any other use of them between the products
-// made the compiler copy them in every tile.)
+// any reference near their scores: a row's is its largest score of the first 32
+// keys that its wave meets, seen by the row or not, and it stays; no later tile is
+// searched for maxima.  A row whose weights add up to less than 2^-60 or more than
+// 2^60 (scores 41 off in natural units), or to no number, whose results are not
+// finite (values above 2^67 may leave fp32's range under sums that large, those
+// near 2^127 under any), or that is hidden from values that are not finite, sends its
+// workgroup through careful_rows, which does the block over, moves references tile by
+// tile and takes the second product's weights times 2^-32 (2^30 keys of equal weight
+// then add up to 2^-2).  Weights under 2^-66 of a row's sum, and products with a value
+// under 2^-66, may leave fp32's range below.  (Kept apart, so that the accumulators
+// have one place throughout: any other use of them between the products made the
+// compiler copy them in every tile.  References 40 log2 units above the scores would
+// spare the look at the results, which takes 0.1-0.7 % of a call, but differences that
+// large round 6 times coarser in lse.)
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -83,10 +83,8 @@ using kc::lds_i16x4;
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLeast = 0x1p-60f, kMost = 0x1p-2f;     // sums that stand
-constexpr float kAbove = 40.0f, kAboveMoved = 32.0f;    // of a fixed / a moved reference, above the scores it is taken from
-constexpr float kAboveFirst = 58.0f;                    // at most above a seen score
-constexpr float kMergeScale = 0x1p-32f;                 // of a merge's weights: any number of finite rows stays finite
+constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;     // sums that stand
+constexpr float kLowered = 0x1p-32f;                    // of the weights of rows that are done over
 constexpr float kUnset = -FLT_MAX;
 
 // Score products accumulate in vector registers, with the queries in accumulation
@@ -397,18 +395,12 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     f32x16 s[KB][G];
     uint32_t w[G][8 * KB];                  // weights, bf16 pairs
     float block_sum[G];
-    int here[G];                            // keys of the tile that the lane's rows see, less 4 half
     // the row's largest score of the tile's first key block, log2 units
     auto top_of = [&](int g) __attribute__((always_inline)) {
         float top = s[0][g][0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][g][i]);
         return max_halves(top) * c2;
-    };
-    // the row's score of its first key
-    auto first_of = [&](int g) __attribute__((always_inline)) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[0][g][0]), __float_as_uint(s[0][g][0]), false, false);
-        return __uint_as_float(r[0]) * c2;
     };
     auto weights = [&](int g, int ks) __attribute__((always_inline)) {
         const u32x4 x = {w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3]};
@@ -478,6 +470,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     // early units start in slot 4 of the value phase (4 products after the scores), the
     // late ones, and the test of the sums, fill the score phase.
     float argument, weight, kept;               // in the units' pipeline
+    int here[G];                                // keys of the tile that the lane's rows see, less 4 half
     auto set_here = [&](int key) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < G; ++g) here[g] = sees_of(cur, r0 + 32 * g + col) - key - 4 * half;
@@ -539,10 +532,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         for (int g = 0; g < G; ++g) scores_ready(s[0][g]);
         if (first) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const float one = first_of(g);      // (a key that scores -inf weighs nothing)
-                ref[g] = fmaxf(kUnset, fminf(top_of(g) + kAbove, here[g] + 4 * half > 0 && one >= kUnset ? one + kAboveFirst : INFINITY));
-            }
+            for (int g = 0; g < G; ++g) ref[g] = fmaxf(kUnset, top_of(g));
         }
 #pragma unroll
         for (int u = 0; u < kEarly; ++u) unit(0, u, true);
@@ -610,13 +600,14 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
     };
 
     // ---- results of the 32 rows from row x of the block on; register i of block m is
-    // channel 32 m + (i & 3) + 8 (i >> 2) + 4 half.  `own`: 8 KiB of LDS for the wave.
-    auto put_rows = [&](int x, f32x16 (&o)[4], float ref, float sum, uint8_t* own) __attribute__((always_inline)) {
+    // channel 32 m + (i & 3) + 8 (i >> 2) + 4 half, times `lowered` to the sum's weights.
+    // `own`: 8 KiB of LDS for the wave.
+    auto put_rows = [&](int x, f32x16 (&o)[4], float ref, float sum, float lowered, uint8_t* own) __attribute__((always_inline)) {
         const int l = fresh_lane(), col = l & 31, half = l >> 5;
         const float total = sum_halves(sum);
         // weights that all vanish leave 0 here; whether that is a row without keys is
         // decided below, by what the row sees
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const float inv = total == 0.0f ? 0.0f : 1.0f / (total * lowered);
         const int r = x + col;
         if (cur.part >= 0) {
             if (r >= min(cur.q_rows, a.part_rows)) return;
@@ -629,10 +620,9 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                     *reinterpret_cast<float4*>(to + 32 * m + 2 * i) = make_float4(o[m][i] * inv, o[m][i + 1] * inv, o[m][i + 2] * inv, o[m][i + 3] * inv);
             if (half == 0) {
                 // a partial that weighs nothing has no reference: a row that sees no key of
-                // the split may have taken its own from keys that it does not see.  Others
-                // are kept as 2^m l with l in [0.5, 1): the largest m is then the merge's.
-                a.part_m[row] = total == 0.0f ? kUnset : ref + static_cast<float>(__builtin_amdgcn_frexp_expf(total));
-                a.part_l[row] = __builtin_amdgcn_frexp_mantf(total);
+                // the split may have taken its own from keys that it does not see
+                a.part_m[row] = total == 0.0f ? kUnset : ref;
+                a.part_l[row] = total;
             }
             return;
         }
@@ -746,7 +736,14 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
         for (int g = 0; g < G; ++g) {
             const float total = sum_halves(sum[g]);
             const int row = r0 + 32 * g + col;
-            careful = careful || __ballot(!(total < kMost && total > kLeast) && row < cur.q_rows && sees_of(cur, row) > cur.key0) != 0;
+            // results that are not finite leave a sum of their products that is not
+            float odd[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) odd[(i >> 1) & 1] = fmaf(acc[g][m][i], acc[g][m][i + 1], odd[(i >> 1) & 1]);
+            const bool stands = total < kMost && total > kLeast && fabsf(odd[0] + odd[1]) < INFINITY;
+            careful = careful || __ballot(!stands && row < cur.q_rows && sees_of(cur, row) > cur.key0) != 0;
         }
         if (lane == 0) flags[S::buffers * NW + wave] = careful;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
@@ -757,7 +754,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
             // in the place of the last tile, which no wave reads any more (the other two
             // are the next block's)
 #pragma unroll
-            for (int g = 0; g < G; ++g) put_rows(r0 + 32 * g, acc[g], ref[g], sum[g], smem + (S::listed ? after(after(off)) : 0) + wave * 32 * 256);
+            for (int g = 0; g < G; ++g) put_rows(r0 + 32 * g, acc[g], ref[g], sum[g], 1.0f, smem + (S::listed ? after(after(off)) : 0) + wave * 32 * 256);
             if (more && cur.tiles == 0) stage_first(following, off);
         } else {
             // careful_rows: 32 rows of a wave at a time, a tile at a time.
@@ -801,7 +798,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                             z[i] = (i & 3) + 8 * (i >> 2) < seen_here ? z[i] : -INFINITY;
                             top = fmaxf(top, z[i]);
                         }
-                        const float to = fminf(fmaxf(rc, max_halves(top) * c2 + kAboveMoved), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
+                        const float to = fminf(fmaxf(rc, max_halves(top) * c2), FLT_MAX);   // (a score of +inf: weight, sum and lse +inf)
                         const float f = __builtin_amdgcn_exp2f(rc - to);
                         rc = to;
                         sc *= f;
@@ -811,7 +808,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                             const float e0 = __builtin_amdgcn_exp2f(fmaf(z[i], c2, -rc)), e1 = __builtin_amdgcn_exp2f(fmaf(z[i + 1], c2, -rc));
                             sc += e0;
                             sc += e1;
-                            pairs[i >> 1] = kc::pack_bf16x2(e0, e1);
+                            pairs[i >> 1] = kc::pack_bf16x2(e0 * kLowered, e1 * kLowered);
                         }
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
@@ -847,7 +844,7 @@ __global__ __launch_bounds__(64 * NW, G == 2 ? 1 : 2) void prefill_kernel(Prefil
                         }
                     }
                 }
-                put_rows(x, o, rc, sc, smem + S::tile + wave * 32 * 256);
+                put_rows(x, o, rc, sc, kLowered, smem + S::tile + wave * 32 * 256);
             }
             if (more) {
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");       // no wave reads the last tile
@@ -875,43 +872,68 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillArgs a) {
     const int part0 = max(g.part0, 0), parts = min(g.num_parts, a.num_parts - part0);
     const int64_t step = static_cast<int64_t>(a.H) * a.part_rows;
     const int64_t row = part0 * step + static_cast<int64_t>(head) * a.part_rows + r;
-    // the loads of eight partials before any is used (a token on 64K keys, 16 heads, 32
-    // splits: a call of 114 us with one after the other, 111 so)
-    float top = kUnset, sum = 0.0f;
-    float2 o = make_float2(0.0f, 0.0f);
-    for (int j0 = 0; j0 < parts; j0 += 8) {
-        float m[8], l[8];
-        float2 x[8];
+    // The row's reference and sum first, then its partials by their share of the sum, so
+    // that finite rows give a finite one (a token on 64K keys, 16 heads, 32 splits: 108 us
+    // a call against 107 in one pass).  The loads of eight partials before any is used (3
+    // us of that call).
+    const auto load = [&](int j0, float (&m)[8], float (&l)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t at = row + min(j0 + i, parts - 1) * step;
             m[i] = a.part_m[at];
             l[i] = a.part_l[at];
-            x[i] = *reinterpret_cast<const float2*>(a.part_o + at * kValue + 2 * lane);
         }
+    };
+    const auto load_rows = [&](int j0, float2 (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = *reinterpret_cast<const float2*>(a.part_o + (row + min(j0 + i, parts - 1) * step) * kValue + 2 * lane);
+    };
+    float top = kUnset, sum = 0.0f;
+    float2 o = make_float2(0.0f, 0.0f);
+    float m0[8], l0[8];
+    float2 x0[8];
+    if (parts > 0) {
+        load(0, m0, l0);
+        load_rows(0, x0);
+    }
+    for (int j0 = 0; j0 < parts; j0 += 8) {
+        float m[8], l[8];
+        if (j0 > 0) load(j0, m, l);
         const float before = top;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, m[i]);
-        const float kept = exp2f(before - top);
-        sum *= kept;
-        o.x *= kept;
-        o.y *= kept;
-#pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (j0 + i >= parts) break;
-            const float f = exp2f(m[i] - top) * (l[i] * kMergeScale);
-            sum += f;
-            o.x = fmaf(f, x[i].x, o.x);
-            o.y = fmaf(f, x[i].y, o.y);
+            m[i] = j0 > 0 ? m[i] : m0[i];
+            l[i] = j0 > 0 ? l[i] : l0[i];
+            top = fmaxf(top, m[i]);
         }
+        sum *= exp2f(before - top);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j0 + i < parts) sum += exp2f(m[i] - top) * l[i];
     }
     const bool none = min(static_cast<int64_t>(g.kv_len), static_cast<int64_t>(g.seen0) + r) <= 0;
     const float inv = none ? 0.0f : 1.0f / sum;
+    for (int j0 = 0; j0 < parts; j0 += 8) {
+        float m[8], l[8];
+        float2 x[8];
+        if (j0 > 0) {
+            load(j0, m, l);
+            load_rows(j0, x);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (j0 + i >= parts) break;
+            const float share = exp2f((j0 > 0 ? m[i] : m0[i]) - top) * (j0 > 0 ? l[i] : l0[i]) * inv;
+            o.x = fmaf(share, j0 > 0 ? x[i].x : x0[i].x, o.x);
+            o.y = fmaf(share, j0 > 0 ? x[i].y : x0[i].y, o.y);
+        }
+    }
     const int64_t q = static_cast<int64_t>(g.q_row) + r;
     *reinterpret_cast<uint32_t*>(a.out + q * a.out_stride_t + static_cast<int64_t>(head) * a.out_stride_h + 2 * lane) =
-        kc::pack_bf16x2(o.x * inv, o.y * inv);
+        kc::pack_bf16x2(o.x, o.y);
     if (a.lse != nullptr && lane == 0)
-        a.lse[q * a.H + head] = none ? -INFINITY : (top + log2f(sum / kMergeScale)) * 0.6931471805599453f;
+        a.lse[q * a.H + head] = none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace

@@ -3,12 +3,16 @@ give finite outputs, whatever weights the values meet on the way -- scores that
 grow by tens of units behind a row's first keys, many keys of equal weight,
 blocks done over, and partials that are merged.
 """
+import math
+
+import numpy as np
 import pytest
 
 from unseen_keys import check_finite_case
 
 pytestmark = pytest.mark.gpu
 
+TAU32 = float(np.float32(1.0 / math.sqrt(192.0)))       # as a call takes it
 SHAPES = [([200], [1500]), ([90], [700]), ([1], [64]), ([3], [5000]), ([257], [3000]), ([1, 2, 1], [3000, 70, 4099])]
 
 
@@ -77,3 +81,40 @@ def check_some_rows(c, what):
                 assert bool(c.out[a + i].isnan().all()) and bool((c.lse[a + i] == -float("inf")).all())
                 c.out[a + i] = 0.0
     check_finite_case(c, range(2), what)
+
+
+@pytest.mark.parametrize("q,kv", [([1], [1]), ([64], [64]), ([200], [300]), ([3], [5000]), ([257], [3000])])
+@pytest.mark.parametrize("grow", [0.0, 60.0])
+def test_lse_keeps_32_bits(q, kv, grow):
+    """Scores that are exact in fp32: lse is as near to the formula's as fp32 takes it, beside references too.
+
+    k is 0 but in one channel of 0 or 1, q in that channel a multiple of 1/8: the products are exact.  In units of 2^-24:
+    softmax_scale log2(e) is off by 2 and the score's difference from the reference rounds by 1, together at most 4 |z|;
+    exp2 2; the sum 1 for every step of the longest chain (16 in a key block, one per key block, one for the halves); the
+    logarithm 2 and the last sum and product 2, of lse; merging adds 2 for a weight and one per partial (the chains' room
+    for it: splits have at least 4 key blocks)."""
+    import torch
+
+    from test_gpu_prefill import TAU, Call
+    c = Call(q, kv, 2, True, seed=25)
+    for t in (c.q_nope, c.q_rope, c.k_nope, c.k_rope):
+        t[:] = 0.0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(26)
+    nq, nk = q[0], kv[0]
+    c.q_nope[:nq, :, 0] = torch.randint(1, 16, (nq, 2), generator=g, device="cuda").bfloat16() / 8.0
+    c.k_nope[:nk, :, 0] = torch.randint(0, 2, (nk, 2), generator=g, device="cuda").bfloat16()
+    if grow:                                            # all but the first 40 keys, by 74: the rows are done over
+        c.q_nope[:nq, :, 1] = 8.0
+        c.k_nope[40:nk, :, 1] = 128.0
+    c.run()
+    torch.cuda.synchronize()
+    for h in range(2):
+        z = TAU32 * (c.q_nope[:nq, h].double() @ c.k_nope[:nk, h].double().T.contiguous())
+        hidden = torch.arange(nk, device="cuda")[None] >= (torch.arange(nq, device="cuda") + nk - nq + 1)[:, None]
+        lse = torch.logsumexp(z.masked_fill(hidden, -float("inf")), 1)
+        size = z.masked_fill(hidden, 0.0).abs().amax(1)
+        bound = 2.0 ** -24 * (4.0 * size + 2.0 + 17.0 + nk / 32.0 + 4.0 * lse.abs() + 2.0)
+        r = float(((c.lse[:nq, h].double() - lse).abs() / bound).max())
+        print(f"  {q} on {kv}, {grow}: lse off by {r:.2f} of its bound", flush=True)
+        assert r <= 1.0
