@@ -8,9 +8,9 @@
 // The bytes written are three times the bytes read, so the work split follows
 // the output: every store instruction writes whole rows.
 //
-// Memory bounds it.  128K rows, 4 bits, caches cold: 41 us, 4.8 TB/s (a copy's rate);
-// one row per wave, its RoPE key left to another, took 71, the same with 4 rows 65
-// and 8 rows 58 (stores past the caches in both).  64K protected 2-bit rows: 27 us.
+// Memory bounds it.  128K rows, 4 bits, over 2.6 GB of inputs and outputs in turn: 42 us,
+// 4.6 TB/s (a copy's rate 4.9); one row per wave, its RoPE key left to another, 80.  64K
+// rows, 0.7 GB in turn: 18.0 us with 4 bits, 24.6 protected, 30.7 from the BF16 cache.
 #include <hip/hip_runtime.h>
 
 #include "internal.h"
@@ -189,7 +189,8 @@ template <int CBITS, bool kProt, bool kPaper>
 hipError_t launch_as(const GatherArgs& a, hipStream_t stream) {
     // Eight rows per wave overlap their chains of loads (row -> page -> codes) and share
     // the search and the RoPE keys' wave, where there are waves enough for the card all
-    // the same (32K rows, 4 bits, caches cold: 13 us against 20; at 16K no difference).
+    // the same (32K rows, 4 bits, caches cold: 12.2 us against 16.6, protected 17.4 against
+    // 18.2; 16K: 9.3 against 12.0, but protected 16.5 against 13.1).
     if (a.n >= kManyRows) return launch_rows<CBITS, kProt, kPaper, kRopeRows>(a, stream);
     return launch_rows<CBITS, kProt, kPaper, 1>(a, stream);
 }

@@ -161,10 +161,12 @@ constexpr Shape kShapes[] = {{128, 512, 4}, {256, 256, 8}};
 
 // Up to 128 rows per sequence the reads of the keys bound the kernel, and two small
 // workgroups per CU overlap each other's beginnings and ends; beyond, a workgroup of
-// 256 rows reads the keys half as often.  Measured, 128 rows / 256 rows: 256 prompts
-// of 64, 64 heads 283 / 575 us; 128 of 128 290 / 398; 64 of 256 391 / 351; 129
-// rows on 16 x 4096 keys 878 / 548; 16 of 1024 734 / 588.  (Workgroups of one wave and
-// 32 rows took as long as 128 rows from 1 to 32 rows, 24 x 2K keys: 154 / 146 us.)
+// 256 rows reads the keys half as often.  Measured, 64 heads, 128 rows / 256 rows: 256
+// prompts of 64 243 / 453 us; 128 of 128 235 / 326; 96 of 192 353 / 323; 64 of 256 301 /
+// 293; 16 of 1024 660 / 493; 128 rows on 16 x 4096 keys 490 / 519, 129 rows 855 / 518.
+// The longest sequence decides for the whole call: one prompt of 1024 beside 255 of 64
+// takes 480 us (two calls, one for each kind, 62 + 241), 512 rows beside 63 single tokens
+// on 2K keys, 32 heads, 481 (49 + 376).
 Shape choose_rows(const Lengths& n) {
     int32_t most = 0;
     for (int32_t b = 0; b < n.B; ++b) most = std::max(most, n.q[b]);

@@ -8,8 +8,8 @@
 // waves come first; the RoPE waves run beside them.
 //
 // Memory bounds it where there are many tokens: 1152 bytes read, as many written dense
-// and 324 (4 bits) packed.  8 x 8K tokens, protected, and their gather: 83 us, caches
-// cold, of 58 at a copy's rate.
+// and 324 (4 bits) packed.  64K tokens, dense rows too, caches cold: 42 us with 4 bits (38
+// at a copy's rate), 54 protected (39), 43 into the BF16 cache (49).
 //
 // The norm: squares of bf16 values are exact in fp64, and the sum of 512 of
 // them is rounded so far below bf16 that the order of the reduction does not
@@ -159,8 +159,9 @@ hipError_t launch_rows(const NormRopeArgs& a, hipStream_t stream) {
 template <int CBITS, bool kProt, bool kPaper>
 hipError_t launch_as(const NormRopeArgs& a, hipStream_t stream) {
     // Two tokens per wave share the root and overlap their loads, where there are waves
-    // enough for the card all the same (64K tokens, 4 bits, protected: 73 us against
-    // 76; 32K: 36 against 39; at 16K and below no difference).
+    // enough for the card all the same (64K tokens, 4 bits, protected: 53 us against
+    // 60; 32K: 29 against 32; 16K: 18.6 against 18.3, unprotected 13.5 against 14.5; below no
+    // difference).
     if (a.append.n >= kManyTokens) return launch_rows<CBITS, kProt, kPaper, 2>(a, stream);
     return launch_rows<CBITS, kProt, kPaper, 1>(a, stream);
 }

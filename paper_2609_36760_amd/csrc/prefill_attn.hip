@@ -33,12 +33,12 @@
 //   128 rows, 32 keys: two workgroups per CU overlap each other; for up to 128 rows
 //     per sequence, where the reads of keys and values are the bound.
 //
-// Measured (MI355X), 256 rows: 8K keys, causal, 128 heads 2.24-2.31 ms, 1190-1230 TFLOP/s of
-// the visible keys' products; 8K x 8K, 64 heads 2.02-2.12 ms, 1300-1360 (all-zero
-// inputs 1.51 ms, 1820: what is left is the power limit, 1.75 GHz).  A tile takes 3.5K
-// cycles for 2.56K of products, a block about 12K beside its tiles.  128 rows: one token on
-// 32 x 2K keys, 32 heads 189 us, 5.7 TB/s; 256 prompts of 64, 64 heads 250 us (245 at a
-// copy's rate).
+// Measured (MI355X), 256 rows: 8K keys, causal, 128 heads 2.2-2.3 ms, 1200-1250 TFLOP/s of
+// the visible keys' products; 8K x 8K, 64 heads 2.11 ms, 1300 (at 1.80 GHz; all-zero
+// inputs, in the same cycles at 2.40 GHz, 1.53 ms: what is left is the power limit).  A
+// tile takes 3.5K cycles for 2.56K of products, a block about 12K beside its tiles.  128
+// rows: one token on 24 x 2K keys, 32 heads 169 us, 165 at a copy's rate; 256 prompts
+// of 64, 64 heads 243 us (245).
 //
 // Roundings: the weights are bf16 operands of the second product (at most 2^-8
 // of a weight, as the bf16 output's own rounding; bf16 values allow no wider
