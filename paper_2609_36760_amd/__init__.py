@@ -1,8 +1,8 @@
 """Low-bit MLA decode for AMD MI355X (gfx950).
 
 The compute lives in ``libmla_lowbit.so`` (HIP kernels behind the C ABI of
-include/mla_lowbit.h and include/mla_prefill.h); ``_binding`` and ``_prefill``
-forward to it with the same names.
+include/mla_lowbit.h, include/mla_prefill.h and include/mla_speculate.h);
+``_binding``, ``_prefill`` and ``_speculate`` forward to it with the same names.
 ``synthetic`` draws seeded inputs; ``runner`` sets up device buffers and
 runs whole decode steps through the binding.  Importing this package does not
 load the library; the first binding call does, and fails loudly if it is not
@@ -20,6 +20,10 @@ _PREFILL_NAMES = (
     "mla_rope_queries", "mla_lowbit_gather", "mla_bf16_gather", "mla_lowbit_gather_protected", "mla_plan_prefill",
     "mla_prefill_attn", "rotation", "rms_norm", "MLA_ROPE_PAIRS", "MLA_ROPE_HALVES",
 )
+_SPECULATE_NAMES = (
+    "mla_tree_split_tokens", "mla_tree_workspace_bytes", "mla_lowbit_tree_attn", "mla_bf16_tree_attn",
+    "mla_verify_workspace_bytes", "mla_verify_tree", "layer_caches", "mla_lowbit_commit", "mla_bf16_commit",
+)
 
 
 def __getattr__(name):
@@ -29,4 +33,7 @@ def __getattr__(name):
     if name in _PREFILL_NAMES:
         from . import _prefill
         return getattr(_prefill, name)
+    if name in _SPECULATE_NAMES:
+        from . import _speculate
+        return getattr(_speculate, name)
     raise AttributeError(name)

@@ -17,11 +17,18 @@
 // weighted row) through LDS, so a row of S splits costs ceil(S / 32)
 // dependent rounds of loads.  An empty split holds
 // zeros and weighs e^{-inf} s = 0.
+//
+// Trees of drafted tokens (kTree): rows are (node, head) of a ragged batch, a
+// split holds s_q * H of them, s_q the most nodes of a sequence; rows past a
+// sequence's own are skipped, and no row before or behind them is written.  A
+// row's sum that is NaN gives NaN, and a sum of nothing 0 and -inf.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
+#include "speculate_internal.h"
 
 namespace mla {
 namespace {
@@ -87,19 +94,20 @@ __device__ __forceinline__ RowState combine_splits(const CombineArgs& a, int r, 
     return st;
 }
 
+template <bool kTree>
 __device__ __forceinline__ void store_row(const CombineArgs& a, int64_t row, const float O[8], float M, float S,
                                           int lane) {
     const float inv = S > 0.0f ? 1.0f / S : 0.0f;
     *reinterpret_cast<uint4*>(a.out + row * kDc + lane * 8) =
         make_uint4(pack_bf16x2(O[0] * inv, O[1] * inv), pack_bf16x2(O[2] * inv, O[3] * inv),
                    pack_bf16x2(O[4] * inv, O[5] * inv), pack_bf16x2(O[6] * inv, O[7] * inv));
-    if (a.lse != nullptr && lane == 0) a.lse[row] = S > 0.0f ? M + logf(S) : -INFINITY;
+    if (a.lse != nullptr && lane == 0) a.lse[row] = (kTree ? S != 0.0f : S > 0.0f) ? M + logf(S) : -INFINITY;
 }
 
 // kShared: one row per workgroup, its splits shared by the four waves (many
 // splits per sequence); else four rows per workgroup, one per wave.
-template <bool kShared, int kBatch>
-__global__ __launch_bounds__(64 * kWaves) void combine_kernel(CombineArgs a) {
+template <bool kShared, int kBatch, bool kTree = false>
+__global__ __launch_bounds__(64 * kWaves) void combine_kernel(std::conditional_t<kTree, TreeCombineArgs, CombineArgs> a) {
     // rows (b * s_q + i) * H + h in 8 contiguous ranges of blocks, range x on
     // XCD x (block id mod 8), the XCD whose decode workgroups wrote most of them
     constexpr int kRows = kShared ? 1 : kWaves;
@@ -110,16 +118,25 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(CombineArgs a) {
     if (blk >= blocks_all) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int rows_per_seq = a.s_q * a.H;
-    const int64_t row = blk * kRows + (kShared ? 0 : wave);
+    int64_t row = blk * kRows + (kShared ? 0 : wave);
     if (!kShared && row >= rows_all) return;
     const int b = static_cast<int>(row / rows_per_seq);
     const int r = static_cast<int>(row % rows_per_seq);
-    const int j0 = a.split_indptr[b];
-    const int j1 = a.split_indptr[b + 1];
+    if constexpr (kTree) {
+        const NodeRange nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q);
+        if (r >= nodes.count * a.H) return;
+        row = static_cast<int64_t>(nodes.first) * a.H + r;
+    }
+    int j0 = a.split_indptr[b];
+    int j1 = a.split_indptr[b + 1];
+    if constexpr (kTree) {
+        j0 = max(j0, 0);
+        j1 = min(j1, a.num_splits);
+    }
 
     if constexpr (!kShared) {
         const RowState st = combine_splits<kBatch>(a, r, rows_per_seq, j0, j1, 0, 1, lane);
-        store_row(a, row, st.o, st.mx, st.s, lane);
+        store_row<kTree>(a, row, st.o, st.mx, st.s, lane);
     } else {
         __shared__ float sh_o[kWaves][8][64];
         __shared__ float sh_ms[kWaves][2];
@@ -146,7 +163,7 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(CombineArgs a) {
                 for (int q = 0; q < 8; ++q) O[q] += c * sh_o[w][q][lane];
             }
         }
-        store_row(a, row, O, M, S, lane);
+        store_row<kTree>(a, row, O, M, S, lane);
     }
 }
 
@@ -165,6 +182,24 @@ hipError_t launch_combine(const CombineArgs& a, int32_t num_splits, hipStream_t 
             hipLaunchKernelGGL((combine_kernel<false, 4>), grid, block, 0, stream, a);
         else
             hipLaunchKernelGGL((combine_kernel<false, 8>), grid, block, 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_tree_combine(const TreeCombineArgs& a, hipStream_t stream) {
+    const int32_t num_splits = a.num_splits;
+    const int64_t rows = static_cast<int64_t>(a.B) * a.s_q * a.H;
+    if (rows == 0) return hipSuccess;
+    if (num_splits >= static_cast<int64_t>(kShare) * a.B) {
+        hipLaunchKernelGGL((combine_kernel<true, 8, true>), dim3(static_cast<unsigned>((rows + 7) / 8 * 8)),
+                           dim3(64 * kWaves), 0, stream, a);
+    } else {
+        const int64_t blocks = (rows + kWaves - 1) / kWaves;
+        const dim3 grid(static_cast<unsigned>((blocks + 7) / 8 * 8)), block(64 * kWaves);
+        if (num_splits <= 4 * static_cast<int64_t>(a.B))
+            hipLaunchKernelGGL((combine_kernel<false, 4, true>), grid, block, 0, stream, a);
+        else
+            hipLaunchKernelGGL((combine_kernel<false, 8, true>), grid, block, 0, stream, a);
     }
     return hipGetLastError();
 }

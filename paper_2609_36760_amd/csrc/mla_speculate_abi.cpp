@@ -1,0 +1,306 @@
+// Host side of the C ABI declared in include/mla_speculate.h: argument
+// validation, the choice of a split size, workspace layout and dispatch.
+//
+// This translation unit is plain C++ (it needs only the HIP runtime API
+// types); every check below runs on the host before any HIP call is made.
+#include "mla_speculate.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <functional>
+#include <queue>
+#include <vector>
+
+#include "abi_checks.h"
+#include "internal.h"
+#include "speculate_internal.h"
+
+namespace {
+
+using namespace mla::abi;
+
+constexpr int64_t kMaxRows = int64_t{1} << 20;          // of one sequence: 32-bit byte offsets in the kernel
+constexpr int64_t kMaxTokens = int64_t{1} << 30;        // of a sequence's page table
+constexpr int64_t kPartialBytes = kDc * 2 + 2 * 4;      // of one row of a split
+constexpr int32_t kMaxGridAxis = 65535;
+
+bool sizes_ok(int32_t max_nodes, int32_t H) {
+    return max_nodes >= 1 && max_nodes <= mla::kMaxNodes && H >= 1 && static_cast<int64_t>(max_nodes) * H <= kMaxRows;
+}
+
+int32_t rows_per_workgroup(int32_t max_nodes, int32_t H) {
+    return static_cast<int64_t>(max_nodes) * H <= 64 ? 64 : mla::kDecodeRowsPerBlock;
+}
+
+bool blocks_fit(int64_t blocks, int64_t threads) { return blocks * threads <= mla::kMaxDispatchItems; }
+
+// Estimated time of a call, us: its work items on the compute units of the XCD
+// that takes them, in order, and the merge.
+double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_wg, int32_t split_tokens) {
+    const double fixed = rows_wg == 64 ? 18.5 : 17.5, per_tile = rows_wg == 64 ? 1.25 : 1.6;
+    const int64_t row_blocks = (rows + rows_wg - 1) / rows_wg;
+    std::vector<double> items;
+    for (int32_t b = 0; b < B; ++b)
+        for (int64_t t = 0; t < seq_lens[b]; t += split_tokens) {
+            const int64_t left = std::min<int64_t>(seq_lens[b] - t, split_tokens);
+            items.push_back(fixed + per_tile * static_cast<double>((left + kTile - 1) / kTile));
+        }
+    const int64_t per_xcd = (static_cast<int64_t>(items.size()) + 7) / 8;
+    double longest = 0.0;
+    for (int64_t x = 0; x < 8; ++x) {
+        std::priority_queue<double, std::vector<double>, std::greater<double>> free;
+        for (int i = 0; i < mla::kCus / 8; ++i) free.push(0.0);
+        const int64_t end = std::min<int64_t>((x + 1) * per_xcd, static_cast<int64_t>(items.size()));
+        for (int64_t w = x * per_xcd; w < end; ++w)
+            for (int64_t r = 0; r < row_blocks; ++r) {
+                const double done = free.top() + items[w];
+                free.pop();
+                free.push(done);
+                longest = std::max(longest, done);
+            }
+    }
+    if (static_cast<int64_t>(items.size()) == B) return longest;
+    // partials written and read at 4 TB/s beside the merge's launch
+    const double bytes = 2.0 * static_cast<double>(items.size()) * static_cast<double>(rows) * kPartialBytes;
+    return longest + 4.0 + bytes / 4e6;
+}
+
+int tree_attn(const mla_cache_format* f, bool lowbit, const uint16_t* q_lat, const uint16_t* q_rope,
+              const void* cache, int64_t num_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+              const int32_t* ctx_lens, const int32_t* cu_nodes, const uint64_t* tree_mask, int32_t num_nodes,
+              int32_t max_nodes, int32_t B, int32_t H, float softmax_scale, int32_t split_tokens,
+              const int32_t* split_indptr, int32_t num_splits, uint16_t* out, float* lse, void* workspace,
+              int64_t workspace_bytes, hipStream_t stream) {
+    const int st = lowbit ? check_lowbit_format(f) : check_shape(f);
+    if (st != MLA_OK) return st;
+    if (B < 0 || num_nodes < 0 || num_pages < 0 || max_pages_per_seq <= 0 || split_tokens < 0 || num_splits < 0 ||
+        max_nodes < 1 || H < 1)
+        return MLA_EINVAL;
+    if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.0f)) return MLA_EINVAL;
+    if (!sizes_ok(max_nodes, H) || split_tokens % kTile != 0) return MLA_ENOTSUP;
+    // positions in 32 bits, those of a split past the longest sequence too
+    if (static_cast<int64_t>(max_pages_per_seq) * f->page_size > kMaxTokens || split_tokens > kMaxTokens) return MLA_ENOTSUP;
+    if (B == 0 || num_nodes == 0) return MLA_OK;
+    if (q_lat == nullptr || q_rope == nullptr || cache == nullptr || block_table == nullptr || ctx_lens == nullptr ||
+        cu_nodes == nullptr || tree_mask == nullptr || out == nullptr || num_pages == 0)
+        return MLA_EINVAL;
+    if (!aligned(cache, 256)) return MLA_EINVAL;
+    if (!aligned(q_lat, 16) || !aligned(q_rope, 16) || !aligned(out, 16)) return MLA_ENOTSUP;
+    const int64_t rows = static_cast<int64_t>(max_nodes) * H;
+    const int64_t num_work = split_tokens == 0 ? B : num_splits;
+    const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
+    if (!blocks_fit(mla::decode_workgroups(num_work, rows, rows_wg), mla::kDecodeThreads)) return MLA_ENOTSUP;
+    if (split_tokens != 0) {
+        if (split_indptr == nullptr) return MLA_EINVAL;
+        const int64_t need = mla_tree_workspace_bytes(num_splits, max_nodes, H);
+        if (need < 0) return MLA_ENOTSUP;
+        if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return MLA_EINVAL;
+        if (!aligned(workspace, 16)) return MLA_ENOTSUP;
+        if (!blocks_fit((B * rows + 7) / 8 * 8, mla::kCombineThreads)) return MLA_ENOTSUP;
+    }
+    mla::TreeArgs a{};
+    a.shape = {rows_wg, 4};
+    a.q_lat = q_lat;
+    a.q_rope = q_rope;
+    a.cache = static_cast<const uint8_t*>(cache);
+    a.num_pages = num_pages;
+    a.block_table = block_table;
+    a.max_pages = max_pages_per_seq;
+    a.seq_lens = ctx_lens;
+    a.B = B;
+    a.s_q = max_nodes;
+    a.H = H;
+    a.scale_log2 = softmax_scale * 1.4426950408889634f;
+    a.split_tokens = split_tokens;
+    a.split_indptr = split_indptr;
+    a.num_work = static_cast<int32_t>(num_work);
+    a.out = out;
+    a.lse = lse;
+    a.g = lowbit ? lowbit_geom(f) : bf16_geom(f);
+    a.cu_nodes = cu_nodes;
+    a.mask = tree_mask;
+    a.num_nodes = num_nodes;
+    if (split_tokens != 0) {
+        const int64_t part_rows = num_splits * rows;
+        a.part_o = static_cast<uint16_t*>(workspace);
+        a.part_m = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + part_rows * kDc * 2);
+        a.part_s = a.part_m + part_rows;
+    }
+    const bool paper = f->meta == MLA_META_PAPER;
+    const mla::CacheKind kind = !lowbit ? mla::KIND_BF16
+                                : f->c_bits == 4 ? (paper ? mla::KIND_C4R4P : mla::KIND_C4R4)
+                                                 : (paper ? mla::KIND_C2R4P : mla::KIND_C2R4);
+    const int launched = hip_status(mla::launch_tree_attn(kind, a, stream));
+    if (launched != MLA_OK || split_tokens == 0) return launched;
+    mla::TreeCombineArgs c{};
+    c.part_m = a.part_m;
+    c.part_s = a.part_s;
+    c.part_o = a.part_o;
+    c.split_indptr = split_indptr;
+    c.B = B;
+    c.s_q = max_nodes;
+    c.H = H;
+    c.out = out;
+    c.lse = lse;
+    c.cu_nodes = cu_nodes;
+    c.num_nodes = num_nodes;
+    c.num_splits = num_splits;
+    return hip_status(mla::launch_tree_combine(c, stream));
+}
+
+int commit(const mla_cache_format* f, bool lowbit, void* const* caches, int32_t num_layers, int64_t num_pages,
+           const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens, const int32_t* path,
+           const int32_t* keep, int32_t max_nodes, int32_t B, int32_t* new_lens, hipStream_t stream) {
+    const int st = lowbit ? check_lowbit_format(f) : check_shape(f);
+    if (st != MLA_OK) return st;
+    if (B < 0 || num_layers < 0 || num_pages < 0 || max_pages_per_seq <= 0 || max_nodes < 1) return MLA_EINVAL;
+    if (max_nodes > mla::kMaxNodes || B > kMaxGridAxis) return MLA_ENOTSUP;
+    if (B == 0 || (num_layers == 0 && new_lens == nullptr)) return MLA_OK;
+    if (ctx_lens == nullptr || path == nullptr || keep == nullptr || new_lens == ctx_lens) return MLA_EINVAL;
+    if (num_layers > 0 && (caches == nullptr || block_table == nullptr || num_pages == 0)) return MLA_EINVAL;
+    if (!blocks_fit(static_cast<int64_t>(B) * std::max(num_layers, 1), 256)) return MLA_ENOTSUP;
+    mla::CommitArgs a{};
+    a.caches = reinterpret_cast<uint8_t* const*>(caches);
+    a.num_layers = num_layers;
+    a.num_pages = num_pages;
+    a.block_table = block_table;
+    a.max_pages = max_pages_per_seq;
+    a.ctx_lens = ctx_lens;
+    a.path = path;
+    a.keep = keep;
+    a.max_nodes = max_nodes;
+    a.B = B;
+    a.new_lens = new_lens;
+    a.g = lowbit ? lowbit_geom(f) : bf16_geom(f);
+    return hip_status(mla::launch_commit(a, lowbit, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t mla_tree_split_tokens(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H) {
+    if (B < 0 || max_nodes < 1 || H < 1 || (B > 0 && seq_lens == nullptr)) return -MLA_EINVAL;
+    if (!sizes_ok(max_nodes, H)) return -MLA_ENOTSUP;
+    int64_t tokens = 0;
+    int32_t longest = 0;
+    for (int32_t b = 0; b < B; ++b) {
+        if (seq_lens[b] < 1) return -MLA_EINVAL;
+        tokens += seq_lens[b];
+        longest = std::max(longest, seq_lens[b]);
+    }
+    const int64_t rows = static_cast<int64_t>(max_nodes) * H;
+    const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
+    const int64_t row_blocks = (rows + rows_wg - 1) / rows_wg;
+    // sizes of about a quarter more each time, as long as there are not far more
+    // workgroups than compute units
+    constexpr int64_t kMostBlocks = 16 * mla::kCus;
+    int32_t best = 0;
+    if (B * row_blocks >= kMostBlocks) return 0;
+    double least = tree_cost(seq_lens, B, rows, rows_wg, std::max(longest, 1));
+    for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) {
+        if ((tokens / s + B) * row_blocks > kMostBlocks) continue;
+        const double cost = tree_cost(seq_lens, B, rows, rows_wg, static_cast<int32_t>(s));
+        if (cost < least) {
+            least = cost;
+            best = static_cast<int32_t>(s);
+        }
+    }
+    return best;
+}
+
+int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t H) {
+    if (num_splits < 0 || !sizes_ok(max_nodes, H)) return -1;
+    return static_cast<int64_t>(num_splits) * max_nodes * H * kPartialBytes;
+}
+
+int mla_lowbit_tree_attn(const mla_cache_format* f, const uint16_t* q_lat, const uint16_t* q_rope, const void* cache,
+                         int64_t num_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                         const int32_t* ctx_lens, const int32_t* cu_nodes, const uint64_t* tree_mask,
+                         int32_t num_nodes, int32_t max_nodes, int32_t B, int32_t H, float softmax_scale,
+                         int32_t split_tokens, const int32_t* split_indptr, int32_t num_splits, uint16_t* out,
+                         float* lse, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    return tree_attn(f, true, q_lat, q_rope, cache, num_pages, block_table, max_pages_per_seq, ctx_lens, cu_nodes,
+                     tree_mask, num_nodes, max_nodes, B, H, softmax_scale, split_tokens, split_indptr, num_splits, out,
+                     lse, workspace, workspace_bytes, stream);
+}
+
+int mla_bf16_tree_attn(const mla_cache_format* f, const uint16_t* q_lat, const uint16_t* q_rope, const void* cache,
+                       int64_t num_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                       const int32_t* ctx_lens, const int32_t* cu_nodes, const uint64_t* tree_mask, int32_t num_nodes,
+                       int32_t max_nodes, int32_t B, int32_t H, float softmax_scale, int32_t split_tokens,
+                       const int32_t* split_indptr, int32_t num_splits, uint16_t* out, float* lse, void* workspace,
+                       int64_t workspace_bytes, hipStream_t stream) {
+    return tree_attn(f, false, q_lat, q_rope, cache, num_pages, block_table, max_pages_per_seq, ctx_lens, cu_nodes,
+                     tree_mask, num_nodes, max_nodes, B, H, softmax_scale, split_tokens, split_indptr, num_splits, out,
+                     lse, workspace, workspace_bytes, stream);
+}
+
+int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab) {
+    if (num_nodes < 0 || B < 0 || vocab < 1 || vocab > mla::kMaxVocab) return -1;
+    return static_cast<int64_t>(num_nodes) * mla::logit_chunks(vocab) * static_cast<int64_t>(sizeof(mla::ChunkStat));
+}
+
+int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stride, int32_t vocab,
+                    const float* draft_probs, int64_t draft_stride, const int32_t* tokens, const int32_t* parents,
+                    const int32_t* cu_nodes, int32_t num_nodes, int32_t max_nodes, int32_t B,
+                    const float* temperature, const float* u_accept, const float* u_draw, int32_t* path,
+                    int32_t* out_tokens, float* logprobs, int32_t* keep, void* workspace, int64_t workspace_bytes,
+                    hipStream_t stream) {
+    if (logits_type != MLA_LOGITS_BF16 && logits_type != MLA_LOGITS_FP32) return MLA_EINVAL;
+    if (vocab < 1 || B < 0 || num_nodes < 0 || max_nodes < 1 || logits_stride < vocab) return MLA_EINVAL;
+    if (draft_probs != nullptr && draft_stride < vocab) return MLA_EINVAL;
+    if (vocab > mla::kMaxVocab || max_nodes > mla::kMaxNodes || B > kMaxGridAxis) return MLA_ENOTSUP;
+    if (B == 0) return MLA_OK;
+    if (cu_nodes == nullptr || path == nullptr || out_tokens == nullptr || keep == nullptr) return MLA_EINVAL;
+    if (num_nodes > 0 && (logits == nullptr || tokens == nullptr || parents == nullptr || u_accept == nullptr ||
+                          u_draw == nullptr))
+        return MLA_EINVAL;
+    if (!aligned(logits, logits_type == MLA_LOGITS_FP32 ? 4 : 2) || !aligned(draft_probs, 4)) return MLA_ENOTSUP;
+    const int64_t need = mla_verify_workspace_bytes(num_nodes, B, vocab);
+    if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return MLA_EINVAL;
+    if (!aligned(workspace, 16)) return MLA_ENOTSUP;
+    const int64_t chunk_groups = (mla::logit_chunks(vocab) + 3) / 4;
+    if (!blocks_fit(chunk_groups * max_nodes * B, 256) || !blocks_fit(B, 1024)) return MLA_ENOTSUP;
+    mla::VerifyArgs a{};
+    a.logits = logits;
+    a.logits_stride = logits_stride;
+    a.fp32 = logits_type == MLA_LOGITS_FP32;
+    a.vocab = vocab;
+    a.draft_probs = draft_probs;
+    a.draft_stride = draft_stride;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.cu_nodes = cu_nodes;
+    a.num_nodes = num_nodes;
+    a.max_nodes = max_nodes;
+    a.B = B;
+    a.temperature = temperature;
+    a.u_accept = u_accept;
+    a.u_draw = u_draw;
+    a.path = path;
+    a.out_tokens = out_tokens;
+    a.logprobs = logprobs;
+    a.keep = keep;
+    a.stats = static_cast<mla::ChunkStat*>(workspace);
+    return hip_status(mla::launch_verify(a, stream));
+}
+
+int mla_lowbit_commit(const mla_cache_format* f, void* const* caches, int32_t num_layers, int64_t num_pages,
+                      const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
+                      const int32_t* path, const int32_t* keep, int32_t max_nodes, int32_t B, int32_t* new_lens,
+                      hipStream_t stream) {
+    return commit(f, true, caches, num_layers, num_pages, block_table, max_pages_per_seq, ctx_lens, path, keep,
+                  max_nodes, B, new_lens, stream);
+}
+
+int mla_bf16_commit(const mla_cache_format* f, void* const* caches, int32_t num_layers, int64_t num_pages,
+                    const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
+                    const int32_t* path, const int32_t* keep, int32_t max_nodes, int32_t B, int32_t* new_lens,
+                    hipStream_t stream) {
+    return commit(f, false, caches, num_layers, num_pages, block_table, max_pages_per_seq, ctx_lens, path, keep,
+                  max_nodes, B, new_lens, stream);
+}
+
+}  // extern "C"
