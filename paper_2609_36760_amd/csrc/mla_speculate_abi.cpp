@@ -239,7 +239,8 @@ int mla_bf16_tree_attn(const mla_cache_format* f, const uint16_t* q_lat, const u
 
 int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab) {
     if (num_nodes < 0 || B < 0 || vocab < 1 || vocab > mla::kMaxVocab) return -1;
-    return static_cast<int64_t>(num_nodes) * mla::logit_chunks(vocab) * static_cast<int64_t>(sizeof(mla::ChunkStat));
+    // statistics of every chunk, sums of a shared pass, and its counters
+    return mla::logit_chunks(vocab) * (num_nodes * int64_t{sizeof(mla::ChunkStat)} + B * int64_t{8}) + B * int64_t{4};
 }
 
 int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stride, int32_t vocab,
@@ -283,7 +284,10 @@ int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stri
     a.out_tokens = out_tokens;
     a.logprobs = logprobs;
     a.keep = keep;
+    const int64_t chunks = mla::logit_chunks(vocab);
     a.stats = static_cast<mla::ChunkStat*>(workspace);
+    a.sums = reinterpret_cast<double*>(a.stats + num_nodes * chunks);
+    a.arrived = reinterpret_cast<int32_t*>(a.sums + B * chunks);
     return hip_status(mla::launch_verify(a, stream));
 }
 

@@ -55,6 +55,8 @@ struct VerifyArgs {
     float* logprobs;
     int32_t* keep;
     ChunkStat* stats;                           // [num_nodes][chunks]
+    double* sums;                               // [B][chunks] of a shared pass
+    int32_t* arrived;                           // [B] workgroups that have done their share of it
 };
 
 // Commit (commit.hip).

@@ -265,5 +265,5 @@ def test_a_graph_and_no_nodes():
     # no rows at all
     none = torch.empty((0, V), device=DEV)
     i0, f0 = torch.empty(0, dtype=torch.int32, device=DEV), torch.empty(0, device=DEV)
-    ms.mla_verify_tree(none, i0, i0, torch.zeros(4, dtype=torch.int32, device=DEV), most, f0, ud, path, out, keep, None)
+    ms.mla_verify_tree(none, i0, i0, torch.zeros(4, dtype=torch.int32, device=DEV), most, f0, ud, path, out, keep, space)
     assert keep.tolist() == [0, 0, 0] and (path == -1).all()
