@@ -22,7 +22,9 @@
  * preconditions; the kernels clamp every index that comes from them into its
  * buffer, or pass over it.  Every call can be captured into a graph, and none
  * needs a length on the host: a plan (split_tokens, split_indptr) made for
- * lengths that a sequence has not reached serves it too.  A workspace holds
+ * lengths that a sequence has not reached serves it too.  Positions count in 32
+ * bits: a page table of more than 2^30 tokens, or a longer split, is refused with
+ * MLA_ENOTSUP.  A workspace holds
  * values only while its call runs; two calls that may overlap need one each.
  *
  * Trees.  Sequence b has the nodes cu_nodes[b] .. cu_nodes[b+1]-1 of the
@@ -72,7 +74,7 @@ int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t 
  *   ctx_lens   device, int32 [B]: tokens before the root, >= 0
  *   tree_mask  device, uint64 [num_nodes]: bit j, node j of the same sequence
  *   H          1 or more, max_nodes * H <= 2^20
- *   split_tokens  0: unsplit, else (at most 2^30, as max_pages_per_seq pages of tokens) the splits of mla_plan_splits over the lengths
+ *   split_tokens  0: unsplit, else the splits of mla_plan_splits over the lengths
  *              with the nodes (split_indptr, num_splits; a sequence's splits past
  *              its length are passed over)
  *   out        device, bf16 [num_nodes][H][d_c];  lse device, fp32 [num_nodes][H] or NULL

@@ -156,6 +156,7 @@ int commit(const mla_cache_format* f, bool lowbit, void* const* caches, int32_t 
     if (st != MLA_OK) return st;
     if (B < 0 || num_layers < 0 || num_pages < 0 || max_pages_per_seq <= 0 || max_nodes < 1) return MLA_EINVAL;
     if (max_nodes > mla::kMaxNodes || B > kMaxGridAxis) return MLA_ENOTSUP;
+    if (static_cast<int64_t>(max_pages_per_seq) * f->page_size > kMaxTokens) return MLA_ENOTSUP;
     if (B == 0 || (num_layers == 0 && new_lens == nullptr)) return MLA_OK;
     if (ctx_lens == nullptr || path == nullptr || keep == nullptr || new_lens == ctx_lens) return MLA_EINVAL;
     if (num_layers > 0 && (caches == nullptr || block_table == nullptr || num_pages == 0)) return MLA_EINVAL;
@@ -263,7 +264,7 @@ int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stri
     if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return MLA_EINVAL;
     if (!aligned(workspace, 16)) return MLA_ENOTSUP;
     const int64_t chunk_groups = (mla::logit_chunks(vocab) + 3) / 4;
-    if (!blocks_fit(chunk_groups * max_nodes * B, 256) || !blocks_fit(B, 1024)) return MLA_ENOTSUP;
+    if (!blocks_fit(chunk_groups * max_nodes * B, 256)) return MLA_ENOTSUP;
     mla::VerifyArgs a{};
     a.logits = logits;
     a.logits_stride = logits_stride;

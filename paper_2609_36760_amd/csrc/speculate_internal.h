@@ -72,6 +72,7 @@ struct CommitArgs {
     int32_t max_nodes, B;
     int32_t* new_lens;
     PageGeom g;
+    int32_t layers_each;                        // layers of a workgroup (set by the launch)
 };
 
 // The nodes of sequence b, kept inside the node-indexed arrays for any values.

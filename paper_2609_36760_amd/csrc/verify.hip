@@ -21,6 +21,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "speculate_internal.h"
 
@@ -28,6 +29,7 @@ namespace mla {
 namespace {
 
 constexpr int kSteps = kLogitChunk / 512;       // pieces of 8 consecutive logits per lane and chunk
+constexpr int kWalk = 512;                      // threads of a walk
 constexpr int kMaxChunks = logit_chunks(kMaxVocab);
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -56,33 +58,65 @@ __device__ __forceinline__ double weight(float l, float m, double scale) {
     return pow2(fmax((static_cast<double>(l) - static_cast<double>(m)) * scale, -2000.0));
 }
 
-// Logits x .. x + 7 of a row, -inf past its end (rows need no alignment beyond
+// Eight consecutive logits as they lie in memory (rows need no alignment beyond
 // their type's).
 template <bool kF32>
-__device__ __forceinline__ void load8(const VerifyArgs& a, int64_t row, int x, float l[8]) {
-    if constexpr (kF32) {
-        const float* p = static_cast<const float*>(a.logits) + row * a.logits_stride + x;
-        if (x + 8 <= a.vocab) {
-            __builtin_memcpy(l, p, 32);
-        } else {
+struct Piece {
+    uint32_t w[kF32 ? 8 : 4];
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (kF32) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    }
+};
+template <bool kF32>
+__device__ __forceinline__ Piece<kF32> load_piece(const VerifyArgs& a, int64_t row, int x) {
+    using T = std::conditional_t<kF32, uint32_t, uint16_t>;
+    Piece<kF32> p;
+    __builtin_memcpy(p.w, static_cast<const T*>(a.logits) + row * a.logits_stride + x, sizeof(p.w));
+    return p;
+}
+// The same where the row may end: -inf behind its end.
+template <bool kF32>
+__device__ __forceinline__ Piece<kF32> load_end(const VerifyArgs& a, int64_t row, int x) {
+    using T = std::conditional_t<kF32, uint32_t, uint16_t>;
+    if (x + 8 <= a.vocab) return load_piece<kF32>(a, row, x);
+    const T* from = static_cast<const T*>(a.logits) + row * a.logits_stride + x;
+    Piece<kF32> p;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) l[i] = x + i < a.vocab ? p[i] : -INFINITY;
-        }
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t l = x + i < a.vocab ? from[i] : kF32 ? 0xFF800000u : 0xFF80u;
+        if constexpr (kF32) p.w[i] = l;
+        else p.w[i >> 1] = i & 1 ? p.w[i >> 1] | l << 16 : l;
+    }
+    return p;
+}
+// A lane's pieces of a chunk.  They go round in their registers, so that loops over
+// them need not be unrolled: the code runs once or twice per wave, and fetching
+// it counts.
+template <class P>
+struct Round {
+    P at[kSteps];
+    __device__ __forceinline__ void next() {
+        const P p = at[0];
+#pragma unroll
+        for (int j = 0; j + 1 < kSteps; ++j) at[j] = at[j + 1];
+        at[kSteps - 1] = p;
+    }
+};
+template <bool kF32>
+__device__ __forceinline__ Round<Piece<kF32>> load_chunk(const VerifyArgs& a, int64_t row, int chunk, int x0) {
+    Round<Piece<kF32>> l;
+    if ((chunk + 1) * kLogitChunk <= a.vocab) {
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) l.at[j] = load_piece<kF32>(a, row, x0 + 512 * j);
     } else {
-        const uint16_t* p = static_cast<const uint16_t*>(a.logits) + row * a.logits_stride + x;
-        if (x + 8 <= a.vocab) {
-            uint32_t w[4];
-            __builtin_memcpy(w, p, 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                l[2 * i] = __uint_as_float(w[i] << 16);
-                l[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) l[i] = x + i < a.vocab ? __uint_as_float(static_cast<uint32_t>(p[i]) << 16) : -INFINITY;
+#pragma unroll 1
+        for (int j = 0; j < kSteps; ++j) {
+            l.at[0] = load_end<kF32>(a, row, x0 + 512 * j);
+            l.next();
         }
     }
+    return l;
 }
 template <bool kF32>
 __device__ __forceinline__ float load1(const VerifyArgs& a, int64_t row, int x) {
@@ -91,21 +125,49 @@ __device__ __forceinline__ float load1(const VerifyArgs& a, int64_t row, int x) 
     else return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.logits)[at]) << 16);
 }
 
+// A value of each lane's partner at distance 1, 2, (mirrored) 4 and 8, 16 and 32: six
+// exchanges without LDS that bring a symmetric operation to all lanes.
+template <int kStep>
+__device__ __forceinline__ uint32_t partner(uint32_t v) {
+    if constexpr (kStep == 0) return __builtin_amdgcn_mov_dpp(static_cast<int>(v), 0xB1, 0xF, 0xF, true);        // quad_perm 1, 0, 3, 2
+    else if constexpr (kStep == 1) return __builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x4E, 0xF, 0xF, true);   // quad_perm 2, 3, 0, 1
+    else if constexpr (kStep == 2) return __builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x141, 0xF, 0xF, true);  // row_half_mirror
+    else if constexpr (kStep == 3) return __builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x140, 0xF, 0xF, true);  // row_mirror
+    else if constexpr (kStep == 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (threadIdx.x & 16) != 0 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return (threadIdx.x & 32) != 0 ? r[0] : r[1];
+    }
+}
+template <int kStep>
+__device__ __forceinline__ double partner(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = partner<kStep>(static_cast<uint32_t>(u)), hi = partner<kStep>(static_cast<uint32_t>(u >> 32));
+    return __builtin_bit_cast(double, hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    v += partner<0>(v);
+    v += partner<1>(v);
+    v += partner<2>(v);
+    v += partner<3>(v);
+    v += partner<4>(v);
+    v += partner<5>(v);
     return v;
 }
 // The largest of a wave's values, NaN if one is.
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = __builtin_elementwise_maximum(v, __shfl_xor(v, d));
-    return v;
+template <int kStep>
+__device__ __forceinline__ float larger(float v) {
+    return __builtin_elementwise_maximum(v, __uint_as_float(partner<kStep>(__float_as_uint(v))));
 }
+__device__ __forceinline__ float wave_max(float v) {
+    return larger<5>(larger<4>(larger<3>(larger<2>(larger<1>(larger<0>(v))))));
+}
+template <int kStep>
+__device__ __forceinline__ int smaller(int v) { return min(v, static_cast<int>(partner<kStep>(static_cast<uint32_t>(v)))); }
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = min(v, __shfl_xor(v, d));
-    return v;
+    return smaller<5>(smaller<4>(smaller<3>(smaller<2>(smaller<1>(smaller<0>(v))))));
 }
 __device__ __forceinline__ double lane_value(double v, int lane) {
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
@@ -120,14 +182,27 @@ __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_am
 
 __device__ __forceinline__ float temperature_of(const VerifyArgs& a, int b) {
     const float t = a.temperature == nullptr ? 1.0f : a.temperature[b];
-    return t > 0.0f ? t : 0.0f;
+    return t > 0.0f ? fminf(t, 1e30f) : 0.0f;
+}
+// log2(e) / t, within 2^-51: a division in fp64 would take as long as the weights
+// of two logits per lane.
+__device__ __forceinline__ double scale_of(float t) {
+    const double d = t;
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    return kLog2e * r;
 }
 
 // ---------------------------------------------------------------------------
-// A wave holds its chunk's 2 048 logits in registers.  Bound by the reads, with
-// the weights close behind: about 20 fp64 instructions a logit.
+// A wave holds its chunk's 2 048 logits in registers.  Bound by its instructions, 17
+// in fp64 and 3 others a logit: 432 rows of 131 072 bf16 logits take 37 us, 19 without
+// the weights (5.9 TB/s), and 35 the instructions at their measured rate.  Tried: a
+// wave that goes through many chunks with the next one's loads on their way (45-58 us:
+// fewer waves fit), weights from a table of 2^(j/32) (the same count), whole parts
+// added to the exponent (the same), exchanges through LDS and a division in fp64 (49).
 template <bool kF32>
-__global__ __launch_bounds__(256) void stats_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) {
     const int lane = threadIdx.x & 63;
     const int chunk = blockIdx.x * 4 + (threadIdx.x >> 6);
     const int node = blockIdx.y, b = blockIdx.z;
@@ -137,32 +212,32 @@ __global__ __launch_bounds__(256) void stats_kernel(VerifyArgs a) {
     if (node >= nodes.count || chunk >= chunks) return;
     const int64_t row = nodes.first + node;
     const float t = temperature_of(a, b);
-    float l[kSteps][8];
     const int x0 = chunk * kLogitChunk + 8 * lane;
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) load8<kF32>(a, row, x0 + 512 * j, l[j]);
+    Round<Piece<kF32>> l = load_chunk<kF32>(a, row, chunk, x0);
     float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = __builtin_elementwise_maximum(m, l[j][i]);
+        for (int i = 0; i < 8; ++i) m = __builtin_elementwise_maximum(m, l.at[j][i]);
     m = wave_max(m);
     double s = 0.0;
     if (!(m < INFINITY)) {
         m = NAN;            // a NaN or +inf: the row cannot be used
     } else if (t == 0.0f) {
         int first = a.vocab;
+#pragma unroll 1
+        for (int j = 0; j < kSteps; ++j) {
 #pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j)
-#pragma unroll
-            for (int i = 7; i >= 0; --i) first = l[j][i] == m ? x0 + 512 * j + i : first;
+            for (int i = 0; i < 8; ++i) first = l.at[0][i] == m ? min(first, x0 + 512 * j + i) : first;
+            l.next();
+        }
         s = wave_min(first);
     } else if (m != -INFINITY) {
-        const double scale = kLog2e / static_cast<double>(t);
+        const double scale = scale_of(t);
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += weight(l[j][i], m, scale);
+            for (int i = 0; i < 8; ++i) s += weight(l.at[j][i], m, scale);
         s = wave_sum(s);
     }
     if (lane == 0) a.stats[row * chunks + chunk] = ChunkStat{s, m, 0.0f};
@@ -177,9 +252,31 @@ struct WalkShared {
     double weight_of[kMaxNodes];        // of a node's token in its parent's row
     double sum[kMaxChunks];             // of the row's chunks, as they are left
     double wave[kThreads / 64];
+    int first[kThreads / 64], final[kThreads / 64];
     double below;
-    int found, last;
+    float logit;
+    int last;
 };
+
+// The smallest `first` and the largest `final` of the workgroup's threads, each
+// growing with the thread where it is set (kNone and -1 where not).
+constexpr int kNone = 0x7FFFFFFF;
+template <int kThreads>
+__device__ __forceinline__ void block_ends(WalkShared<kThreads>& sh, int& first, int& final) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(first != kNone), any = __builtin_amdgcn_ballot_w64(final >= 0);
+    // (read before the branch: the values of lanes outside it need not be there)
+    const int lowest = __builtin_amdgcn_readlane(first, some != 0 ? __builtin_ctzll(some) : 0);
+    const int highest = __builtin_amdgcn_readlane(final, any != 0 ? 63 - __builtin_clzll(any) : 0);
+    if (lane == 0) {
+        sh.first[wave] = lowest;
+        sh.final[wave] = highest;
+    }
+    __syncthreads();
+    first = wave_min(lane < kThreads / 64 ? sh.first[lane] : kNone);
+    final = -wave_min(lane < kThreads / 64 ? -sh.final[lane] : 1);
+    __syncthreads();
+}
 
 // Inclusive sum over the workgroup's threads, and the whole sum.
 template <int kThreads>
@@ -208,8 +305,8 @@ __device__ __forceinline__ double block_scan(WalkShared<kThreads>& sh, double v,
 // first pass over a row.  Each lane of every wave holds one node, and every
 // wave walks by itself.
 template <bool kF32, bool kSampled>
-__global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs a) {
-    constexpr int kThreads = kSampled ? 1024 : 512, kWaves = kThreads / 64;
+__global__ __launch_bounds__(kWalk, 4) void walk_kernel(VerifyArgs a) {
+    constexpr int kThreads = kWalk, kWaves = kThreads / 64;
     __shared__ WalkShared<kThreads> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.y;
@@ -217,7 +314,7 @@ __global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs 
     const int n = nodes.count, V = a.vocab, chunks = logit_chunks(V);
     const float t = temperature_of(a, b);
     const bool greedy = t == 0.0f;
-    const double scale = greedy ? 0.0 : kLog2e / static_cast<double>(t);
+    const double scale = greedy ? 0.0 : scale_of(t);
 
     // this lane's node: its parent, its token and what decides about it
     int parent = -1, token = -1;
@@ -278,41 +375,45 @@ __global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs 
 
     // weights of a chunk as they are left, summed by a wave
     auto chunk_sum = [&](int c, int64_t row, float m) {
-        float l[kSteps][8];
         double s = 0.0;
         const int x0 = c * kLogitChunk + 8 * lane;
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) load8<kF32>(a, row, x0 + 512 * j, l[j]);
+        Round<Piece<kF32>> l = load_chunk<kF32>(a, row, c, x0);
+        Round<Piece<true>> q;               // the drafting model's probabilities (0 past the row's end)
         if constexpr (kSampled) {
-            const float* q = a.draft_probs + row * a.draft_stride;
+            const float* from = a.draft_probs + row * a.draft_stride;
+            if ((c + 1) * kLogitChunk <= V) {
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-                const int x = x0 + 512 * j;
-                float d[8];
-                if (x + 8 <= V) {
-                    __builtin_memcpy(d, q + x, 32);
-                } else {
+                for (int j = 0; j < kSteps; ++j) __builtin_memcpy(q.at[j].w, from + x0 + 512 * j, sizeof(q.at[j].w));
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < kSteps; ++j) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = x + i < V ? q[x + i] : 0.0f;
+                    for (int i = 0; i < 8; ++i)
+                        q.at[0].w[i] = x0 + 512 * j + i < V ? __float_as_uint(from[x0 + 512 * j + i]) : 0u;
+                    q.next();
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    s += fmax(__builtin_fma(-cut, static_cast<double>(d[i]), weight(l[j][i], m, scale)), 0.0);
             }
-        } else {
+        }
+#pragma unroll 1
+        for (int j = 0; j < kSteps; ++j) {
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int x = x0 + 512 * j + i;
-                    bool out = false;
-                    for (uint64_t r = rejected; r != 0; r &= r - 1) out |= lane_value(token, __builtin_ctzll(r)) == x;
-                    s += out ? 0.0 : weight(l[j][i], m, scale);
+            for (int i = 0; i < 8; ++i) {
+                double w = weight(l.at[0][i], m, scale);
+                if constexpr (kSampled) {
+                    w = fmax(__builtin_fma(-cut, static_cast<double>(q.at[0][i]), w), 0.0);
+                } else {
+                    for (uint64_t r = rejected; r != 0; r &= r - 1)
+                        w = lane_value(token, __builtin_ctzll(r)) == x0 + 512 * j + i ? 0.0 : w;
                 }
+                s += w;
+            }
+            l.next();
+            if constexpr (kSampled) q.next();
         }
         return wave_sum(s);
     };
 
+    double* const shared_sums = a.sums + static_cast<int64_t>(b) * chunks;
     while (n > 0) {
         my_path = lane == keep ? v : my_path;
         ++keep;
@@ -353,16 +454,20 @@ __global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs 
                     __syncthreads();
                     for (int c = share * kWaves + wave; c < chunks; c += shares * kWaves) {
                         const double s = chunk_sum(c, row, m);
-                        if (lane == 0) (shares > 1 ? a.sums + static_cast<int64_t>(b) * chunks : sh.sum)[c] = s;
+                        if (lane == 0 && shares > 1) __hip_atomic_store(&shared_sums[c], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        if (lane == 0 && shares <= 1) sh.sum[c] = s;
                     }
                     if (shares > 1) {
-                        __threadfence();
+                        // (stores and loads that pass the caches between the XCDs; a fence of
+                        // the whole card by every wave costs 100 us here)
+                        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                         __syncthreads();
-                        if (tid == 0) sh.last = atomicAdd(&a.arrived[b], 1) == shares - 1;
+                        if (tid == 0)
+                            sh.last = __hip_atomic_fetch_add(&a.arrived[b], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
                         __syncthreads();
                         if (sh.last == 0) return;
-                        __threadfence();
-                        for (int c = tid; c < chunks; c += kThreads) sh.sum[c] = a.sums[static_cast<int64_t>(b) * chunks + c];
+                        for (int c = tid; c < chunks; c += kThreads)
+                            sh.sum[c] = __hip_atomic_load(&shared_sums[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                     }
                     passed = true;
                     __syncthreads();
@@ -417,11 +522,16 @@ __global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs 
                 } else {
                     for (int c = tid; c < chunks; c += kThreads) sh.sum[c] = st[c].sum * weight(st[c].max, m, scale);
                     __syncthreads();
+                    // chunks with tokens that were not taken: less their weights, or, where
+                    // that would leave too few digits, summed again without them
                     int j = 0;
                     for (uint64_t r = rejected; r != 0; r &= r - 1, ++j) {
                         if (j % kWaves != wave) continue;
                         const int c = lane_value(token, __builtin_ctzll(r)) / kLogitChunk;
-                        const double s = chunk_sum(c, row, m);
+                        const bool here = ((rejected >> lane) & 1) != 0 && token / kLogitChunk == c;
+                        const double before = st[c].sum * weight(st[c].max, m, scale);
+                        double s = before - wave_sum(here ? my_weight : 0.0);
+                        if (!(s > 0x1p-14 * before)) s = chunk_sum(c, row, m);
                         if (lane == 0) sh.sum[c] = s;       // (several tokens of a chunk: the same)
                     }
                 }
@@ -438,67 +548,61 @@ __global__ __launch_bounds__(kSampled ? 1024 : 512) void walk_kernel(VerifyArgs 
                 cut = 0.0;
             }
             const double target = fmax(static_cast<double>(a.u_draw[b]), 0.0) * all;
-            if (tid == 0) {
-                sh.found = kMaxChunks;
-                sh.last = 0;
-            }
-            __syncthreads();
             // the first chunk that passes the target (for a number of 1, or NaN, the last with weight)
             double at = up - sum;
+            int first = kNone, final = -1;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 at += mine[i];
-                if (mine[i] > 0.0) atomicMax(&sh.last, tid * kEach + i);
-                if (mine[i] > 0.0 && at > target) atomicMin(&sh.found, tid * kEach + i);
+                if (mine[i] > 0.0) final = tid * kEach + i;
+                if (mine[i] > 0.0 && at > target && first == kNone) first = tid * kEach + i;
             }
-            __syncthreads();
-            const int c = sh.found < kMaxChunks ? sh.found : sh.last;
+            block_ends(sh, first, final);
+            const int c = first != kNone ? first : max(final, 0);
             at = up - sum;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 if (tid * kEach + i == c) sh.below = at;
                 at += mine[i];
             }
-            __syncthreads();
             // its tokens, consecutive ones per thread
             constexpr int kTokens = kLogitChunk / kThreads;
             double ws[kTokens];
+            float ls[kTokens];
             const int y0 = c * kLogitChunk + tid * kTokens;
             sum = 0.0;
 #pragma unroll
             for (int i = 0; i < kTokens; ++i) {
                 const int y = y0 + i;
-                ws[i] = 0.0;
-                if (y < V) {
-                    ws[i] = weight(load1<kF32>(a, row, y), m, scale);
-                    if constexpr (kSampled) {
-                        if (cut > 0.0)
-                            ws[i] = fmax(__builtin_fma(-cut, static_cast<double>(a.draft_probs[row * a.draft_stride + y]), ws[i]), 0.0);
-                    } else {
-                        for (uint64_t r = rejected; r != 0; r &= r - 1)
-                            if (lane_value(token, __builtin_ctzll(r)) == y) ws[i] = 0.0;
-                    }
+                ls[i] = y < V ? load1<kF32>(a, row, y) : -INFINITY;
+                ws[i] = weight(ls[i], m, scale);
+                if constexpr (kSampled) {
+                    if (cut > 0.0 && y < V)
+                        ws[i] = fmax(__builtin_fma(-cut, static_cast<double>(a.draft_probs[row * a.draft_stride + y]), ws[i]), 0.0);
+                } else {
+                    for (uint64_t r = rejected; r != 0; r &= r - 1)
+                        ws[i] = lane_value(token, __builtin_ctzll(r)) == y ? 0.0 : ws[i];
                 }
                 sum += ws[i];
             }
-            at = sh.below;
             up = block_scan(sh, sum, all);
-            if (tid == 0) {
-                sh.found = V;
-                sh.last = -1;
-            }
-            __syncthreads();
-            at += up - sum;
+            at = sh.below + up - sum;
+            first = kNone;
+            final = -1;
 #pragma unroll
             for (int i = 0; i < kTokens; ++i) {
                 at += ws[i];
-                if (ws[i] > 0.0) atomicMax(&sh.last, y0 + i);
-                if (ws[i] > 0.0 && at > target) atomicMin(&sh.found, y0 + i);
+                if (ws[i] > 0.0) final = y0 + i;
+                if (ws[i] > 0.0 && at > target && first == kNone) first = y0 + i;
             }
-            __syncthreads();
+            block_ends(sh, first, final);
             // (the target may lie behind the tokens' own sum, by its rounding)
-            x = sh.found < V ? sh.found : sh.last;
-            w = x >= 0 ? weight(load1<kF32>(a, row, x), m, scale) : 1.0;
+            x = first != kNone ? first : final;
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i)
+                if (y0 + i == x) sh.logit = ls[i];
+            __syncthreads();
+            w = x >= 0 ? weight(sh.logit, m, scale) : 1.0;
         }
         if (lane == keep - 1) {
             my_out = x;
@@ -524,11 +628,11 @@ void launch(const VerifyArgs& a, hipStream_t stream) {
     }
     if (a.draft_probs != nullptr) {
         // workgroups that share a pass: no more than fill the card once, nor than there are chunks for their waves
-        const int most = (chunks + 15) / 16, share = kCus / a.B;
+        const int most = (chunks + kWalk / 64 - 1) / (kWalk / 64), share = 2 * kCus / a.B;
         const int g = a.num_nodes == 0 ? 1 : share < 1 ? 1 : share < most ? share : most;
-        hipLaunchKernelGGL((walk_kernel<kF32, true>), dim3(g, a.B), dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((walk_kernel<kF32, true>), dim3(g, a.B), dim3(kWalk), 0, stream, a);
     } else {
-        hipLaunchKernelGGL((walk_kernel<kF32, false>), dim3(1, a.B), dim3(512), 0, stream, a);
+        hipLaunchKernelGGL((walk_kernel<kF32, false>), dim3(1, a.B), dim3(kWalk), 0, stream, a);
     }
 }
 
