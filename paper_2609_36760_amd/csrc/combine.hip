@@ -21,7 +21,8 @@
 // Trees of drafted tokens (kTree): rows are (node, head) of a ragged batch, a
 // split holds s_q * H of them, s_q the most nodes of a sequence; rows past a
 // sequence's own are skipped, and no row before or behind them is written.  A
-// row's sum that is NaN gives NaN, and a sum of nothing 0 and -inf.
+// row's sum that is NaN gives NaN, and a sum of nothing 0 and -inf.  Sequences of
+// one split have none to merge.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -130,6 +131,7 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(std::conditional_t
     int j0 = a.split_indptr[b];
     int j1 = a.split_indptr[b + 1];
     if constexpr (kTree) {
+        if (j1 - j0 == 1) return;       // the attention wrote the rows itself
         j0 = max(j0, 0);
         j1 = min(j1, a.num_splits);
     }
@@ -167,6 +169,49 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(std::conditional_t
     }
 }
 
+// Rows of a tree launch.  Where a batch is ragged most rows that the sizes allow do
+// not exist, or need no merge; as many waves as the card holds go through those that
+// do, found by the lanes' sequences (up to 64 of them; larger batches go through
+// all rows).  24 sequences of up to 32 nodes at 128 heads: @ us, 35 with a wave for
+// every row that may exist (bound by being started), 35 with one for every eight.
+template <int kBatch>
+__global__ __launch_bounds__(64 * kWaves) void tree_rows_kernel(TreeCombineArgs a) {
+    const int rows_per_seq = a.s_q * a.H;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * kWaves + wave, step = static_cast<int64_t>(gridDim.x) * kWaves;
+    auto merge = [&](int first, int r, int j0, int j1) {
+        const RowState st = combine_splits<kBatch>(a, r, rows_per_seq, max(j0, 0), min(j1, a.num_splits), 0, 1, lane);
+        store_row<true>(a, static_cast<int64_t>(first) * a.H + r, st.o, st.mx, st.s, lane);
+    };
+    if (a.B > 64) {
+        for (int64_t row = from; row < static_cast<int64_t>(a.B) * rows_per_seq; row += step) {
+            const int b = static_cast<int>(row / rows_per_seq), r = static_cast<int>(row % rows_per_seq);
+            const NodeRange nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q);
+            const int j0 = a.split_indptr[b], j1 = a.split_indptr[b + 1];
+            // (of one split, the attention wrote the rows itself)
+            if (r < nodes.count * a.H && j1 - j0 != 1) merge(nodes.first, r, j0, j1);
+        }
+        return;
+    }
+    const int b = min(lane, a.B - 1);
+    const NodeRange nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q);
+    const int j0 = a.split_indptr[b], j1 = a.split_indptr[b + 1];
+    const int rows = lane < a.B && j1 - j0 != 1 ? nodes.count * a.H : 0;
+    int to = rows;                      // rows up to this lane's last
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(to, d);
+        to += lane >= d ? o : 0;
+    }
+    const int all = __builtin_amdgcn_readlane(to, 63);
+    for (int64_t i = from; i < all; i += step) {
+        const int at = static_cast<int>(i);
+        const int pick = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= at));
+        merge(__builtin_amdgcn_readlane(nodes.first, pick), at - __builtin_amdgcn_readlane(to - rows, pick),
+              __builtin_amdgcn_readlane(j0, pick), __builtin_amdgcn_readlane(j1, pick));
+    }
+}
+
 }  // namespace
 
 hipError_t launch_combine(const CombineArgs& a, int32_t num_splits, hipStream_t stream) {
@@ -195,11 +240,11 @@ hipError_t launch_tree_combine(const TreeCombineArgs& a, hipStream_t stream) {
                            dim3(64 * kWaves), 0, stream, a);
     } else {
         const int64_t blocks = (rows + kWaves - 1) / kWaves;
-        const dim3 grid(static_cast<unsigned>((blocks + 7) / 8 * 8)), block(64 * kWaves);
+        const dim3 grid(static_cast<unsigned>(blocks < 8 * kCus ? blocks : 8 * kCus)), block(64 * kWaves);
         if (num_splits <= 4 * static_cast<int64_t>(a.B))
-            hipLaunchKernelGGL((combine_kernel<false, 4, true>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((tree_rows_kernel<4>), grid, block, 0, stream, a);
         else
-            hipLaunchKernelGGL((combine_kernel<false, 8, true>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((tree_rows_kernel<8>), grid, block, 0, stream, a);
     }
     return hipGetLastError();
 }

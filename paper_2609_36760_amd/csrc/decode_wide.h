@@ -638,6 +638,96 @@ __device__ __forceinline__ void clean_tile(uint8_t* tile, uint8_t* flags, int ti
 // are the last ones of a sequence; in them the hidden keys' scores are -inf, and
 // the tile is looked over first (clean_tile): a key with a channel that is not
 // finite would reach the rows that do not see it as 0 x NaN in the aggregation.
+// What a workgroup of a tree launch works on.  The launch has as many as the plan's
+// splits would need if every sequence had the most rows; the ones that have work
+// come first.  Runs of eight of them are dealt out to the XCDs (block id mod 8), so
+// that row blocks of one split, or splits of one sequence, share their keys or
+// queries in an L2, and no XCD has much more to do than another.
+// The items of a batch end together only if the short ones come last: up to 64
+// sequences (one per lane) the whole splits of all sequences come first, then
+// their last ones, the longest first, then those that a plan for longer sequences
+// has and that hold nothing.  Larger batches keep the sequences' order.
+// 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads: @ us, 625 with whole
+// splits dealt out, 632 in the sequences' order, 670 with contiguous ranges of
+// splits per XCD.
+struct TreeItem {
+    int b, split, rb;
+    int context;
+    int part;           // place of its partials, in the sequences' order
+    bool alone;         // the sequence has no other split
+    bool some;          // false: nothing to do
+};
+template <int kRows>
+__device__ __forceinline__ TreeItem tree_item(const TreeArgs& a, int lane) {
+    const int run = static_cast<int>(blockIdx.x / (8 * kTreeRun)) * 8 + static_cast<int>(blockIdx.x & 7);
+    const int p = kTreeRun * run + static_cast<int>((blockIdx.x >> 3) % kTreeRun);
+    const bool splits = a.split_tokens != 0;
+    if (a.B > 64) {
+        const int blocks = (a.s_q * a.H + kRows - 1) / kRows, w = p / blocks;
+        TreeItem item{w, 0, p % blocks, 0, w, true, w < a.num_work};
+        if (!item.some) return item;
+        if (splits) {
+            // the last sequence whose splits begin at or before w
+            int last = -1;
+            for (int base = 0; base < a.B; base += 64) {
+                const int begin = base + lane < a.B ? a.split_indptr[base + lane] : 0x7FFFFFFF;
+                last += __builtin_popcountll(__builtin_amdgcn_ballot_w64(begin <= w));
+            }
+            item.b = min(max(last, 0), a.B - 1);
+            item.split = w - a.split_indptr[item.b];
+            item.alone = a.split_indptr[item.b + 1] - a.split_indptr[item.b] == 1;
+        }
+        item.context = a.seq_lens[item.b];
+        return item;
+    }
+    // this lane's sequence: its row blocks, splits, and whole splits
+    const int b = min(lane, a.B - 1);
+    const int context = a.seq_lens[b], nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q).count;
+    const int length = max(context, 0) + nodes;
+    const int begin = splits ? a.split_indptr[b] : 0;
+    const int planned = splits ? a.split_indptr[b + 1] - begin : 1;
+    const int blocks = lane < a.B ? (nodes * a.H + kRows - 1) / kRows : 0;
+    const int count = min(max(planned, 0), a.num_work);
+    const int whole = splits ? min(length / a.split_tokens, count) : 0;
+    const int rest = count > whole ? length - whole * (splits ? a.split_tokens : 0) : -1;      // -1: no last split
+    // sums over the lanes before this one
+    auto before = [&](int v) {
+        int up = v;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(up, d);
+            up += lane >= d ? o : 0;
+        }
+        return up - v;
+    };
+    // the workgroups of a lane's whole splits, last split and empty splits: first one and number
+    const int n0 = whole * blocks, n1 = rest >= 0 ? blocks : 0, n2 = max(count - whole - 1, 0) * blocks;
+    const int at0 = before(n0), all0 = __builtin_amdgcn_readlane(at0 + n0, 63);
+    int at1 = all0, all1 = all0;
+    for (int i = 0; i < a.B; ++i) {     // last splits that are longer, or equal and before this lane's
+        const int other = __builtin_amdgcn_readlane(rest, i), n = __builtin_amdgcn_readlane(n1, i);
+        at1 += other > rest || (other == rest && i < lane) ? n : 0;
+        all1 += n;
+    }
+    const int at2 = all1 + before(n2);
+    const int in0 = p - at0, in1 = p - at1, in2 = p - at2;
+    const bool is0 = in0 >= 0 && in0 < n0, is1 = in1 >= 0 && in1 < n1, is2 = in2 >= 0 && in2 < n2;
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(is0 || is1 || is2);
+    TreeItem item{0, 0, 0, 0, 0, true, hit != 0};
+    if (hit == 0) return item;
+    const int in = is0 ? in0 : is1 ? in1 : in2;
+    const int split = (is0 ? 0 : is1 ? whole : whole + 1) + (blocks > 0 ? in / blocks : 0);
+    const int rb = blocks > 0 ? in % blocks : 0;
+    const int pick = __builtin_ctzll(hit);
+    item.b = pick;
+    item.split = __builtin_amdgcn_readlane(split, pick);
+    item.rb = __builtin_amdgcn_readlane(rb, pick);
+    item.context = __builtin_amdgcn_readlane(context, pick);
+    item.part = min(max(__builtin_amdgcn_readlane(begin, pick) + item.split, 0), a.num_work - 1);
+    item.alone = __builtin_amdgcn_readlane(planned, pick) == 1;
+    return item;
+}
+
 template <bool kTree> using KernelArgs = std::conditional_t<kTree, TreeArgs, DecodeArgs>;
 
 template <int KIND, bool kProt, int kTS, bool kTree = false>
@@ -674,13 +764,25 @@ void decode_kernel(KernelArgs<kTree> a) {
     // (which read the same tiles).
     const int per_xcd = (a.num_work + 7) / 8;
     const int slot = blockIdx.x >> 3;
-    const int w = (blockIdx.x & 7) * per_xcd + slot / RB;
-    const int rb = slot % RB;
-    if (w >= a.num_work) return;
+    int w = (blockIdx.x & 7) * per_xcd + slot / RB;
+    int rb = slot % RB;
+    [[maybe_unused]] TreeItem item{};
+    if constexpr (kTree) {
+        item = tree_item<kRowsPerBlock>(a, lane);
+        if (!item.some) return;
+        w = item.part;
+        rb = item.rb;
+    } else {
+        if (w >= a.num_work) return;
+    }
 
     const int P = a.g.page_size;
     int b, split = 0, Lraw;
-    if (a.split_tokens == 0) {
+    if constexpr (kTree) {
+        b = item.b;
+        split = item.split;
+        Lraw = item.context;
+    } else if (a.split_tokens == 0) {
         b = w;
         Lraw = a.seq_lens[b];
     } else {
@@ -703,7 +805,6 @@ void decode_kernel(KernelArgs<kTree> a) {
             cnt += c;
         }
         b = min(cnt - 1, a.B - 1);
-        if constexpr (kTree) b = max(b, 0);
         split = w - start;
     }
     int L = min(max(Lraw, 0), a.max_pages * P);
@@ -1379,7 +1480,8 @@ void decode_kernel(KernelArgs<kTree> a) {
     // pitch (the 16-byte shift per row spreads the 32 rows of a write over the
     // banks), then reads them back row by row.
     float l_tot = sum_halves(l_run);
-    const bool split_out = a.split_tokens != 0;
+    bool split_out = a.split_tokens != 0;
+    if constexpr (kTree) split_out = split_out && !item.alone;
     const float inv = l_tot > 0.0f ? 1.0f / l_tot : 0.0f;
     __syncthreads();        // every wave is done with the tiles (no staging load is in flight)
     const int row0 = rb * kRowsPerBlock + rw * 32;      // the wave's rows of the output, or of work item w's partials

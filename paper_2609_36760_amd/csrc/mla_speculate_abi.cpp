@@ -46,13 +46,11 @@ double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_
             const int64_t left = std::min<int64_t>(seq_lens[b] - t, split_tokens);
             items.push_back(fixed + per_tile * static_cast<double>((left + kTile - 1) / kTile));
         }
-    const int64_t per_xcd = (static_cast<int64_t>(items.size()) + 7) / 8;
     double longest = 0.0;
     for (int64_t x = 0; x < 8; ++x) {
         std::priority_queue<double, std::vector<double>, std::greater<double>> free;
         for (int i = 0; i < mla::kCus / 8; ++i) free.push(0.0);
-        const int64_t end = std::min<int64_t>((x + 1) * per_xcd, static_cast<int64_t>(items.size()));
-        for (int64_t w = x * per_xcd; w < end; ++w)
+        for (size_t w = static_cast<size_t>(x); w < items.size(); w += 8)
             for (int64_t r = 0; r < row_blocks; ++r) {
                 const double done = free.top() + items[w];
                 free.pop();
@@ -90,7 +88,7 @@ int tree_attn(const mla_cache_format* f, bool lowbit, const uint16_t* q_lat, con
     const int64_t rows = static_cast<int64_t>(max_nodes) * H;
     const int64_t num_work = split_tokens == 0 ? B : num_splits;
     const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
-    if (!blocks_fit(mla::decode_workgroups(num_work, rows, rows_wg), mla::kDecodeThreads)) return MLA_ENOTSUP;
+    if (!blocks_fit(mla::tree_workgroups(num_work, rows, rows_wg), mla::kDecodeThreads)) return MLA_ENOTSUP;
     if (split_tokens != 0) {
         if (split_indptr == nullptr) return MLA_EINVAL;
         const int64_t need = mla_tree_workspace_bytes(num_splits, max_nodes, H);

@@ -75,6 +75,12 @@ struct CommitArgs {
     int32_t layers_each;                        // layers of a workgroup (set by the launch)
 };
 
+// Workgroups of its launch: padded so that runs of kTreeRun go round the 8 XCDs.
+constexpr int kTreeRun = 8;
+constexpr int64_t tree_workgroups(int64_t num_work, int64_t rows, int64_t rows_per_block) {
+    return (num_work * ((rows + rows_per_block - 1) / rows_per_block) + 8 * kTreeRun - 1) / (8 * kTreeRun) * (8 * kTreeRun);
+}
+
 // The nodes of sequence b, kept inside the node-indexed arrays for any values.
 struct NodeRange {
     int32_t first, count;

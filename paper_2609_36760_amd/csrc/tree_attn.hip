@@ -7,7 +7,7 @@ namespace {
 
 template <int KIND>
 void launch_kind(const TreeArgs& a, hipStream_t stream) {
-    const int64_t blocks = decode_workgroups(a.num_work, static_cast<int64_t>(a.s_q) * a.H, a.shape.rows);
+    const int64_t blocks = tree_workgroups(a.num_work, static_cast<int64_t>(a.s_q) * a.H, a.shape.rows);
     const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
     if (a.shape.rows == rows_per_block(2)) hipLaunchKernelGGL((decode_kernel<KIND, false, 2, true>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((decode_kernel<KIND, false, 1, true>), grid, block, 0, stream, a);
