@@ -640,16 +640,16 @@ __device__ __forceinline__ void clean_tile(uint8_t* tile, uint8_t* flags, int ti
 // finite would reach the rows that do not see it as 0 x NaN in the aggregation.
 // What a workgroup of a tree launch works on.  The launch has as many as the plan's
 // splits would need if every sequence had the most rows; the ones that have work
-// come first.  Runs of eight of them are dealt out to the XCDs (block id mod 8), so
+// come first.  Runs of them (tree_run) are dealt out to the XCDs (block id mod 8), so
 // that row blocks of one split, or splits of one sequence, share their keys or
 // queries in an L2, and no XCD has much more to do than another.
 // The items of a batch end together only if the short ones come last: up to 64
 // sequences (one per lane) the whole splits of all sequences come first, then
 // their last ones, the longest first, then those that a plan for longer sequences
 // has and that hold nothing.  Larger batches keep the sequences' order.
-// 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads: @ us, 625 with whole
-// splits dealt out, 632 in the sequences' order, 670 with contiguous ranges of
-// splits per XCD.
+// 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads: 510 us, 625 with splits
+// dealt out instead of row blocks, 632 so and in the sequences' order, 670 with
+// contiguous ranges of splits per XCD.
 struct TreeItem {
     int b, split, rb;
     int context;
@@ -659,8 +659,9 @@ struct TreeItem {
 };
 template <int kRows>
 __device__ __forceinline__ TreeItem tree_item(const TreeArgs& a, int lane) {
-    const int run = static_cast<int>(blockIdx.x / (8 * kTreeRun)) * 8 + static_cast<int>(blockIdx.x & 7);
-    const int p = kTreeRun * run + static_cast<int>((blockIdx.x >> 3) % kTreeRun);
+    const int each = tree_run((a.s_q * a.H + kRows - 1) / kRows);
+    const int run = static_cast<int>(blockIdx.x >> 3) / each * 8 + static_cast<int>(blockIdx.x & 7);
+    const int p = each * run + static_cast<int>(blockIdx.x >> 3) % each;
     const bool splits = a.split_tokens != 0;
     if (a.B > 64) {
         const int blocks = (a.s_q * a.H + kRows - 1) / kRows, w = p / blocks;

@@ -35,33 +35,37 @@ int32_t rows_per_workgroup(int32_t max_nodes, int32_t H) {
 
 bool blocks_fit(int64_t blocks, int64_t threads) { return blocks * threads <= mla::kMaxDispatchItems; }
 
-// Estimated time of a call, us: its work items on the compute units of the XCD
-// that takes them, in order, and the merge.
-double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_wg, int32_t split_tokens) {
+// Estimated time of a call, us: its work items on the compute units in the order of
+// the launch (whole splits, then the last ones of the sequences, the longest
+// first), and the merge.  `mixed`: 0, or sequences of an eighth to all of the rows,
+// which ones goes by the number.
+double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_wg, int64_t split_tokens, int mixed) {
     const double fixed = rows_wg == 64 ? 18.5 : 17.5, per_tile = rows_wg == 64 ? 1.25 : 1.6;
-    const int64_t row_blocks = (rows + rows_wg - 1) / rows_wg;
-    std::vector<double> items;
-    for (int32_t b = 0; b < B; ++b)
-        for (int64_t t = 0; t < seq_lens[b]; t += split_tokens) {
-            const int64_t left = std::min<int64_t>(seq_lens[b] - t, split_tokens);
-            items.push_back(fixed + per_tile * static_cast<double>((left + kTile - 1) / kTile));
-        }
-    double longest = 0.0;
-    for (int64_t x = 0; x < 8; ++x) {
-        std::priority_queue<double, std::vector<double>, std::greater<double>> free;
-        for (int i = 0; i < mla::kCus / 8; ++i) free.push(0.0);
-        for (size_t w = static_cast<size_t>(x); w < items.size(); w += 8)
-            for (int64_t r = 0; r < row_blocks; ++r) {
-                const double done = free.top() + items[w];
-                free.pop();
-                free.push(done);
-                longest = std::max(longest, done);
-            }
+    const auto tiles = [](int64_t n) { return static_cast<double>((n + kTile - 1) / kTile); };
+    struct Item { double time; int64_t blocks; };
+    std::vector<Item> items, last;
+    double partial_rows = 0.0;
+    for (int32_t b = 0; b < B; ++b) {
+        const int64_t own = mixed > 0 ? (rows * ((b * 5 + mixed) % 8 + 1) + 7) / 8 : rows, blocks = (own + rows_wg - 1) / rows_wg;
+        const int64_t whole = seq_lens[b] / split_tokens, left = seq_lens[b] % split_tokens;
+        if (whole > 0) items.push_back({fixed + per_tile * tiles(split_tokens), whole * blocks});
+        if (left > 0) last.push_back({fixed + per_tile * tiles(left), blocks});
+        if (seq_lens[b] > split_tokens) partial_rows += static_cast<double>(own * (whole + (left > 0 ? 1 : 0)));
     }
-    if (static_cast<int64_t>(items.size()) == B) return longest;
+    std::sort(last.begin(), last.end(), [](const Item& x, const Item& y) { return x.time > y.time; });
+    items.insert(items.end(), last.begin(), last.end());
+    std::priority_queue<double, std::vector<double>, std::greater<double>> free;
+    for (int i = 0; i < mla::kCus; ++i) free.push(0.0);
+    double longest = 0.0;
+    for (const Item& item : items)
+        for (int64_t r = 0; r < item.blocks; ++r) {
+            const double done = free.top() + item.time;
+            free.pop();
+            free.push(done);
+            longest = std::max(longest, done);
+        }
     // partials written and read at 4 TB/s beside the merge's launch
-    const double bytes = 2.0 * static_cast<double>(items.size()) * static_cast<double>(rows) * kPartialBytes;
-    return longest + 4.0 + bytes / 4e6;
+    return partial_rows == 0.0 ? longest : longest + 4.0 + 2.0 * partial_rows * kPartialBytes / 4e6;
 }
 
 int tree_attn(const mla_cache_format* f, bool lowbit, const uint16_t* q_lat, const uint16_t* q_rope,
@@ -189,24 +193,35 @@ int32_t mla_tree_split_tokens(const int32_t* seq_lens, int32_t B, int32_t max_no
         tokens += seq_lens[b];
         longest = std::max(longest, seq_lens[b]);
     }
-    const int64_t rows = static_cast<int64_t>(max_nodes) * H;
+    if (B == 0) return 0;
     const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
-    const int64_t row_blocks = (rows + rows_wg - 1) / rows_wg;
-    // sizes of about a quarter more each time, as long as there are not far more
-    // workgroups than compute units
+    // How many nodes the sequences have is not known here.  Sequences of one length are
+    // taken to have the most, others to be a mixed batch, for which the estimate says
+    // little about single sizes: there the smallest size within 4 % of the best one is
+    // taken, whose items end closer together.
+    bool mixed = false;
+    for (int32_t b = 1; b < B; ++b) mixed = mixed || seq_lens[b] != seq_lens[0];
+    const int64_t rows = static_cast<int64_t>(max_nodes) * H, row_blocks = (rows + rows_wg - 1) / rows_wg;
+    // unsplit, sizes of about a quarter more each time, and even parts of the longest
+    // sequence, as long as there are not far more workgroups than compute units
     constexpr int64_t kMostBlocks = 16 * mla::kCus;
-    int32_t best = 0;
     if (B * row_blocks >= kMostBlocks) return 0;
-    double least = tree_cost(seq_lens, B, rows, rows_wg, std::max(longest, 1));
-    for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) {
-        if ((tokens / s + B) * row_blocks > kMostBlocks) continue;
-        const double cost = tree_cost(seq_lens, B, rows, rows_wg, static_cast<int32_t>(s));
-        if (cost < least) {
-            least = cost;
-            best = static_cast<int32_t>(s);
-        }
+    std::vector<int64_t> sizes{(int64_t{longest} + kTile - 1) / kTile * kTile};
+    for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) sizes.push_back(s);
+    for (int64_t parts = 2; parts <= 32; ++parts) sizes.push_back((longest + parts * kTile - 1) / (parts * kTile) * kTile);
+    std::vector<double> times;
+    for (size_t i = 0; i < sizes.size(); ++i) {
+        const bool no = i > 0 && (sizes[i] >= longest || (tokens / sizes[i] + B) * row_blocks > kMostBlocks);
+        double time = 0.0;
+        for (int k = mixed ? 1 : 0; !no && k < (mixed ? 8 : 1); k += 3)
+            time += tree_cost(seq_lens, B, rows, rows_wg, sizes[i], k);
+        times.push_back(no ? HUGE_VAL : time);
     }
-    return best;
+    const double best = *std::min_element(times.begin(), times.end());
+    size_t pick = sizes.size();
+    for (size_t i = 0; i < sizes.size(); ++i)
+        if (times[i] <= (mixed ? 1.04 : 1.0) * best && (pick == sizes.size() || sizes[i] < sizes[pick])) pick = i;
+    return pick == 0 ? 0 : static_cast<int32_t>(sizes[pick]);
 }
 
 int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t H) {

@@ -75,10 +75,20 @@ struct CommitArgs {
     int32_t layers_each;                        // layers of a workgroup (set by the launch)
 };
 
-// Workgroups of its launch: padded so that runs of kTreeRun go round the 8 XCDs.
-constexpr int kTreeRun = 8;
+// Its workgroups go round the 8 XCDs in runs: the row blocks of a split where they
+// are up to 8, else an even part of them of at most 8.
+#if defined(__HIPCC__)
+__host__ __device__
+#endif
+constexpr int tree_run(int row_blocks) {
+    if (row_blocks <= 2) return 4;
+    const int parts = (row_blocks + 7) / 8;
+    return (row_blocks + parts - 1) / parts;
+}
+// Workgroups of its launch: padded to whole rounds of runs.
 constexpr int64_t tree_workgroups(int64_t num_work, int64_t rows, int64_t rows_per_block) {
-    return (num_work * ((rows + rows_per_block - 1) / rows_per_block) + 8 * kTreeRun - 1) / (8 * kTreeRun) * (8 * kTreeRun);
+    const int64_t blocks = (rows + rows_per_block - 1) / rows_per_block, round = 8 * tree_run(static_cast<int>(blocks));
+    return (num_work * blocks + round - 1) / round * round;
 }
 
 // The nodes of sequence b, kept inside the node-indexed arrays for any values.
