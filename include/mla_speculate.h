@@ -24,8 +24,8 @@
  * needs a length on the host: a plan (split_tokens, split_indptr) made for
  * lengths that a sequence has not reached serves it too.  Positions count in 32
  * bits: a page table of more than 2^30 tokens, or a longer split, is refused with
- * MLA_ENOTSUP.  A workspace holds
- * values only while its call runs; two calls that may overlap need one each.
+ * MLA_ENOTSUP.  A workspace holds values only while its call runs; two calls that
+ * may overlap need one each.
  *
  * Trees.  Sequence b has the nodes cu_nodes[b] .. cu_nodes[b+1]-1 of the
  * node-indexed arrays (device, int32 [B+1], non-decreasing from 0, the last at
@@ -118,7 +118,9 @@ int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab);
  * token is drawn from r: the first x with r(0) + .. + r(x) > u_draw[b] * sum(r)
  * (temperature 0: the largest logit's).  A walk that meets a row of logits with
  * a NaN, with +inf or with nothing above -inf ends there with the token -1.
- * Tokens outside [0, vocab) are never taken.
+ * Tokens outside [0, vocab) are never taken.  Where r has no weight left (the
+ * fixed drafts name every token of p, or the last token's share is lost to
+ * rounding), the token is drawn from p.
  * Everything is computed in fp64 from the logits as they are (relative errors
  * of the weights below 1e-13), so that an outcome differs from exact
  * arithmetic's only where a random number lies that close to a border.
@@ -129,7 +131,7 @@ int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab);
  *   parents      device, int32 [num_nodes]: a node's parent in its sequence, below
  *                the node's own index (else the node is never reached; a root's is
  *                not read)
- *   temperature  device, fp32 [B], >= 0, or NULL (1 for all)
+ *   temperature  device, fp32 [B], >= 0 (above 1e30: as 1e30), or NULL (1 for all)
  *   u_accept     device, fp32 [num_nodes], u_draw device, fp32 [B]: in [0, 1)
  *   path         device, int32 [B][max_nodes]: the nodes that stay, the root first, then -1
  *   out_tokens   device, int32 [B][max_nodes]: the emitted tokens (the taken children's,

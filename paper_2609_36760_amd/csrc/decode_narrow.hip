@@ -1,6 +1,6 @@
 // Decode attention in workgroups of 16 or 32 query rows: the regime of 16 heads
 // and one query token (Appendix F.1, "Native Attention") or of 32 rows, where
-// the kernels of decode_attn.hip would leave most of every matrix instruction
+// the kernels of decode_wide.h would leave most of every matrix instruction
 // idle, and launches of few work items at any number of rows, where they would
 // leave most of the chip idle (choose_shape in internal.h).  Same computation and results contract:
 // absorbed MLA scores z_t = tau (q_lat . C_hat_t + q_rope . K_hat_t), softmax,
@@ -37,7 +37,7 @@
 // BF16 rows (the BF16 cache, and protected rows from a protection buffer) are
 // staged raw into a padded tile of 16 tokens and feed both products directly.
 //
-// Online softmax as in decode_attn.hip: a per-row reference (log2 units) that
+// Online softmax as in decode_wide.h: a per-row reference (log2 units) that
 // moves only when a tile exceeds it by more than 2^10, the accumulators
 // rescaled on the move; the true maximum is tracked for the split partials.
 //
@@ -242,7 +242,7 @@ __device__ __forceinline__ void zero_offsets(f16x2 zz, f16x2* zo) {
 
 // In-launch append (the writer of mla_lowbit_quant_append / mla_bf16_append,
 // and under protection of mla_lowbit_quant_append_protected, for the step's
-// new tokens), as in decode_attn.hip: the wave that reads a new token
+// new tokens), as in decode_wide.h: the wave that reads a new token
 // (`reads(p)`: its part of the key range, or under protection of the key list,
 // holds position p; every row block writes the same bytes itself) writes it
 // before it loads any tile -- the packed copy (BF16:
@@ -335,7 +335,7 @@ void narrow_kernel(DecodeArgs a) {
     const int RB = (rows_total + kR - 1) / kR;
 
     // Block -> (work item, row block): contiguous work items per XCD (block
-    // id mod 8), as in decode_attn.hip.
+    // id mod 8), as in decode_wide.h.
     const int per_xcd = (a.num_work + 7) / 8;
     const int slot = blockIdx.x >> 3;
     const int w = (blockIdx.x & 7) * per_xcd + slot / RB;
@@ -351,7 +351,7 @@ void narrow_kernel(DecodeArgs a) {
     } else {
         // the last b with split_indptr[b] <= w, counted 64 entries at a time
         // with the lengths loaded alongside: one round of loads instead of a
-        // chain of dependent ones (as in decode_attn.hip)
+        // chain of dependent ones (as in decode_wide.h)
         int cnt = 0, start = 0;
         Lraw = 0;
         for (int base = 0; base <= a.B; base += 64) {
@@ -404,7 +404,7 @@ void narrow_kernel(DecodeArgs a) {
     auto tr_read = [](const uint8_t* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p); };
 
     // One phase over keys [t_begin, t_end) in one representation (see
-    // decode_attn.hip): PK is the cache kind whose pipeline runs; kRing reads
+    // decode_wide.h): PK is the cache kind whose pipeline runs; kRing reads
     // bf16 rows of the protection buffer.  This lane's row sees keys
     // t_lo <= t < lim; every valid row sees t < full_lim.
     auto run = [&](auto kind_c, auto ring_c, const int t_begin, const int t_end, const int t_lo, const int lim,

@@ -49,7 +49,7 @@ enum CacheKind { KIND_C4R4 = 0, KIND_C2R4 = 1, KIND_BF16 = 2, KIND_C4R4P = 3, KI
 
 // Query rows and waves of a workgroup: 16 or 32 rows (decode_narrow.hip: one,
 // two or four waves on one row block, each with its part of the keys), or 64 or
-// 128 (decode_attn.hip: four waves on one tile).
+// 128 (decode_wide.h: four waves on one tile).
 struct LaunchShape {
     int32_t rows, waves;
 };
@@ -124,7 +124,7 @@ hipError_t launch_decode_narrow_protected(CacheKind kind, const DecodeArgs& a, h
 // cannot be expressed: the host refuses such shapes before any HIP call.
 constexpr int64_t kMaxDispatchItems = 0xFFFFFFFFll;
 constexpr int kWaveThreads = 64;
-constexpr int kDecodeThreads = 256;          // decode_attn.hip: 4 waves per workgroup
+constexpr int kDecodeThreads = 256;          // decode_wide.h: 4 waves per workgroup
 constexpr int kDecodeRowsPerBlock = 128;     // query rows of its widest shape
 constexpr int kNarrowThreads = 64;           // decode_narrow.hip in its largest launch: one wave per workgroup
 constexpr int kNarrowRowsPerBlock = 16;      // of 16 rows

@@ -1,4 +1,4 @@
-// Device helpers shared by the decode kernels (decode_attn.hip, decode_narrow.hip).
+// Device helpers shared by the decode kernels (decode_wide.h, decode_narrow.hip).
 // Internal; not part of the public C ABI.
 #pragma once
 

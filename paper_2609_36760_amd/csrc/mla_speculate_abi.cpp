@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <exception>
 #include <functional>
 #include <queue>
 #include <vector>
@@ -66,6 +67,44 @@ double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_
         }
     // partials written and read at 4 TB/s beside the merge's launch
     return partial_rows == 0.0 ? longest : longest + 4.0 + 2.0 * partial_rows * kPartialBytes / 4e6;
+}
+
+int32_t split_size(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H) {
+    int64_t tokens = 0;
+    int32_t longest = 0;
+    for (int32_t b = 0; b < B; ++b) {
+        tokens += seq_lens[b];
+        longest = std::max(longest, seq_lens[b]);
+    }
+    if (B == 0) return 0;
+    const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
+    // How many nodes the sequences have is not known here.  Sequences of one length are
+    // taken to have the most, others to be a mixed batch, for which the estimate says
+    // little about single sizes: there the smallest size within 4 % of the best one is
+    // taken, whose items end closer together.
+    bool mixed = false;
+    for (int32_t b = 1; b < B; ++b) mixed = mixed || seq_lens[b] != seq_lens[0];
+    const int64_t rows = static_cast<int64_t>(max_nodes) * H, row_blocks = (rows + rows_wg - 1) / rows_wg;
+    // unsplit, sizes of about a quarter more each time, and even parts of the longest
+    // sequence, as long as there are not far more workgroups than compute units
+    constexpr int64_t kMostBlocks = 16 * mla::kCus;
+    if (B * row_blocks >= kMostBlocks) return 0;
+    std::vector<int64_t> sizes{(int64_t{longest} + kTile - 1) / kTile * kTile};
+    for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) sizes.push_back(s);
+    for (int64_t parts = 2; parts <= 32; ++parts) sizes.push_back((longest + parts * kTile - 1) / (parts * kTile) * kTile);
+    std::vector<double> times;
+    for (size_t i = 0; i < sizes.size(); ++i) {
+        const bool no = i > 0 && (sizes[i] >= longest || (tokens / sizes[i] + B) * row_blocks > kMostBlocks);
+        double time = 0.0;
+        for (int k = mixed ? 1 : 0; !no && k < (mixed ? 8 : 1); k += 3)
+            time += tree_cost(seq_lens, B, rows, rows_wg, sizes[i], k);
+        times.push_back(no ? HUGE_VAL : time);
+    }
+    const double best = *std::min_element(times.begin(), times.end());
+    size_t pick = sizes.size();
+    for (size_t i = 0; i < sizes.size(); ++i)
+        if (times[i] <= (mixed ? 1.04 : 1.0) * best && (pick == sizes.size() || sizes[i] < sizes[pick])) pick = i;
+    return pick == 0 ? 0 : static_cast<int32_t>(sizes[pick]);
 }
 
 int tree_attn(const mla_cache_format* f, bool lowbit, const uint16_t* q_lat, const uint16_t* q_rope,
@@ -186,42 +225,13 @@ extern "C" {
 int32_t mla_tree_split_tokens(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H) {
     if (B < 0 || max_nodes < 1 || H < 1 || (B > 0 && seq_lens == nullptr)) return -MLA_EINVAL;
     if (!sizes_ok(max_nodes, H)) return -MLA_ENOTSUP;
-    int64_t tokens = 0;
-    int32_t longest = 0;
-    for (int32_t b = 0; b < B; ++b) {
+    for (int32_t b = 0; b < B; ++b)
         if (seq_lens[b] < 1) return -MLA_EINVAL;
-        tokens += seq_lens[b];
-        longest = std::max(longest, seq_lens[b]);
+    try {
+        return split_size(seq_lens, B, max_nodes, H);
+    } catch (const std::exception&) {       // no memory for the estimate: any size is a right one
+        return 0;
     }
-    if (B == 0) return 0;
-    const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
-    // How many nodes the sequences have is not known here.  Sequences of one length are
-    // taken to have the most, others to be a mixed batch, for which the estimate says
-    // little about single sizes: there the smallest size within 4 % of the best one is
-    // taken, whose items end closer together.
-    bool mixed = false;
-    for (int32_t b = 1; b < B; ++b) mixed = mixed || seq_lens[b] != seq_lens[0];
-    const int64_t rows = static_cast<int64_t>(max_nodes) * H, row_blocks = (rows + rows_wg - 1) / rows_wg;
-    // unsplit, sizes of about a quarter more each time, and even parts of the longest
-    // sequence, as long as there are not far more workgroups than compute units
-    constexpr int64_t kMostBlocks = 16 * mla::kCus;
-    if (B * row_blocks >= kMostBlocks) return 0;
-    std::vector<int64_t> sizes{(int64_t{longest} + kTile - 1) / kTile * kTile};
-    for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) sizes.push_back(s);
-    for (int64_t parts = 2; parts <= 32; ++parts) sizes.push_back((longest + parts * kTile - 1) / (parts * kTile) * kTile);
-    std::vector<double> times;
-    for (size_t i = 0; i < sizes.size(); ++i) {
-        const bool no = i > 0 && (sizes[i] >= longest || (tokens / sizes[i] + B) * row_blocks > kMostBlocks);
-        double time = 0.0;
-        for (int k = mixed ? 1 : 0; !no && k < (mixed ? 8 : 1); k += 3)
-            time += tree_cost(seq_lens, B, rows, rows_wg, sizes[i], k);
-        times.push_back(no ? HUGE_VAL : time);
-    }
-    const double best = *std::min_element(times.begin(), times.end());
-    size_t pick = sizes.size();
-    for (size_t i = 0; i < sizes.size(); ++i)
-        if (times[i] <= (mixed ? 1.04 : 1.0) * best && (pick == sizes.size() || sizes[i] < sizes[pick])) pick = i;
-    return pick == 0 ? 0 : static_cast<int32_t>(sizes[pick]);
 }
 
 int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t H) {

@@ -1,6 +1,6 @@
 // Device helpers of the quantize-and-append writer, shared by the writer
 // kernels (quant_append.hip) and the decode kernel's in-launch append
-// (decode_attn.hip).  Internal; not part of the public C ABI.
+// (decode_wide.h).  Internal; not part of the public C ABI.
 //
 // Quantizer: Appendix C.4, "Affine group quantization" -- per token, groups of
 // 64 consecutive channels, m = 2^b - 1,

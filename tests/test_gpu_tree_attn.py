@@ -156,6 +156,32 @@ def test_hidden_keys_that_are_not_finite(kind, H, split):
     b.check(split, bad)
 
 
+@pytest.mark.parametrize("kind,split,longer", [("c4", 0, 0), ("c4", 64, 0), ("bf16", 32, 40), ("c2p", 96, 500)])
+def test_more_sequences_than_lanes(kind, split, longer):
+    """70 sequences (the launch finds its work another way up to 64), a plan for longer ones too."""
+    rng = np.random.default_rng(split)
+    ctx = rng.integers(0, 200, 70).tolist()
+    b = Batch(71, kind, 16, ctx, trees(6, rng.integers(0, 7, 70).tolist()), behind=2)
+    b.call(**b.plan(split, lens=[n + longer for n in b.lens] if longer else None))
+    b.check(split)
+
+
+def test_as_many_sequences_as_lanes():
+    rng = np.random.default_rng(1)
+    b = Batch(72, "c4", 20, rng.integers(0, 300, 64).tolist(), trees(7, rng.integers(0, 9, 64).tolist()))
+    for split in (0, 32, 128):
+        b.out.fill_(-77.0)
+        b.call(**b.plan(split, lens=[n + 50 for n in b.lens]))
+        b.check(split)
+
+
+def test_many_splits_of_few_sequences():
+    """16 splits and more per sequence: the merge shares a row's splits between waves."""
+    b = Batch(73, "c4", 16, [900, 40, 1500], trees(8, [9, 3, 30]), behind=1)
+    b.call(**b.plan(32))
+    b.check(32)
+
+
 def test_large_scores_and_spread_weights():
     """Scores far from one another, in both directions along the keys: the reference has to move."""
     for gain in (8.0, 0.02):

@@ -125,6 +125,25 @@ def test_ties_masked_logits_and_rows_that_cannot_be_used(heat, sampled):
     assert got[1][3, 0] == -1 and got[1][4, 0] == -1 and got[1][5, 0] == -1 and got[2][3] == 1
 
 
+@pytest.mark.parametrize("sampled", [False, True])
+@pytest.mark.parametrize("heat", [1e-45, 1e-30, 1e-3, 50.0, 1e30, 3e38, math.inf])
+def test_temperatures(heat, sampled):
+    c, rng = drafted(17, [5] * 6, 3000, sampled=sampled)
+    check(run(**c, temperature=[heat] * 6), **c, temperature=[heat] * 6)
+
+
+def test_the_largest_vocabulary():
+    V = 1 << 21
+    g = torch.Generator().manual_seed(1)
+    logits = torch.randn((3, V), generator=g).bfloat16()
+    logits[:, V - 1] = 16.0
+    c = dict(logits=logits, tokens=np.array([0, V - 1, 7]), parents=[[-1, 0, 1]], u_accept=np.array([0.5, 0.2, 0.9], np.float32),
+             u_draw=np.array([0.7], np.float32))
+    check(run(**c), **c)
+    c["probs"] = torch.softmax(logits.float() * 0.9, 1)
+    check(run(**c), **c)
+
+
 def test_a_bad_row_in_the_middle_of_a_walk():
     V = 64
     logits = torch.zeros((3, V))
