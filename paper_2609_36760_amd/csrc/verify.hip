@@ -36,9 +36,7 @@ constexpr double kLog2e = 1.4426950408889634074;
 // 2^y for y in [-2000, 0]: y = k + f with f in [-1/2, 1/2], 2^f by a polynomial of
 // degree 9 through the Chebyshev points of that interval (relative error below
 // 2e-14; 1 at f = 0).
-__device__ __forceinline__ double pow2(double y) {
-    const double k = __builtin_rint(y);
-    const double f = y - k;
+__device__ __forceinline__ double pow2_part(double f) {
     double p = 0x1.b6571de2f2351p-24;
     p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
     p = __builtin_fma(p, f, 0x1.ffcb76789860fp-17);
@@ -48,8 +46,11 @@ __device__ __forceinline__ double pow2(double y) {
     p = __builtin_fma(p, f, 0x1.c6b08d7044119p-5);
     p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
     p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
-    p = __builtin_fma(p, f, 1.0);
-    return __builtin_ldexp(p, static_cast<int>(k));
+    return __builtin_fma(p, f, 1.0);
+}
+__device__ __forceinline__ double pow2(double y) {
+    const double k = __builtin_rint(y);
+    return __builtin_ldexp(pow2_part(y - k), static_cast<int>(k));
 }
 
 // Weight of logit l <= m beside a finite maximum m; scale = log2(e) / T.  A logit
@@ -195,12 +196,13 @@ __device__ __forceinline__ double scale_of(float t) {
 }
 
 // ---------------------------------------------------------------------------
-// A wave holds its chunk's 2 048 logits in registers.  Bound by its instructions, 17
-// in fp64 and 3 others a logit: 432 rows of 131 072 bf16 logits take 37 us, 19 without
-// the weights (5.9 TB/s), and 35 the instructions at their measured rate.  Tried: a
-// wave that goes through many chunks with the next one's loads on their way (45-58 us:
-// fewer waves fit), weights from a table of 2^(j/32) (the same count), whole parts
-// added to the exponent (the same), exchanges through LDS and a division in fp64 (49).
+// A wave holds its chunk's 2 048 logits in registers.  Bound by its instructions, 14
+// in fp64 and 3 others a logit: 432 rows of 131 072 bf16 logits take 39 us in steady
+// state (2.9 TB/s; 19 us without the weights).  Weights by their definition, 18 and 3
+// instructions, took 47 us where these take 42 (the first 60 launches).  Tried: a wave
+// that goes through many chunks with the next one's loads on their way (a fifth slower:
+// fewer waves fit), weights from a table of 2^(j/32) (no fewer instructions), exchanges
+// through LDS and a division in fp64 (a third slower).
 template <bool kF32>
 __global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) {
     const int lane = threadIdx.x & 63;
@@ -233,12 +235,34 @@ __global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) 
         }
         s = wave_min(first);
     } else if (m != -INFINITY) {
-        const double scale = scale_of(t);
+        const double scale = scale_of(t), top = m * scale;
+        if (fabs(top) <= 0x1p20) {
+            // beside 2^K, K the whole number next to the maximum's exponent: then a logit's
+            // whole part k - K lies in the low bits of l scale + (1.5 2^52 - K), the rest is
+            // one exact product and difference away, and p 2^(k - K) joins the sum in one step.
+            // Logits below the maximum by 2^-140 or more weigh that (2^-129 of the sum for all).
+            const double whole = __builtin_rint(top), magic = 0x1.8p52 - whole;
+            const float lowest = static_cast<float>(static_cast<double>(m) - 140.0 * static_cast<double>(t));
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j)
+            for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += weight(l.at[j][i], m, scale);
-        s = wave_sum(s);
+                for (int i = 0; i < 8; ++i) {
+                    const double x = __builtin_elementwise_maximum(l.at[j][i], lowest);
+                    const double at = __builtin_fma(x, scale, magic);
+                    const double p = pow2_part(__builtin_fma(x, scale, magic - at));
+                    const uint32_t k = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, at));
+                    s = __builtin_fma(p, __builtin_bit_cast(double, static_cast<uint64_t>((k << 20) + 0x3FF00000u) << 32), s);
+                }
+            s = wave_sum(s) * pow2(__builtin_fma(-static_cast<double>(m), scale, whole));
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < kSteps; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += weight(l.at[0][i], m, scale);
+                l.next();
+            }
+            s = wave_sum(s);
+        }
     }
     if (lane == 0) a.stats[row * chunks + chunk] = ChunkStat{s, m, 0.0f};
 }
