@@ -144,6 +144,17 @@ def test_the_largest_vocabulary():
     check(run(**c), **c)
 
 
+@pytest.mark.parametrize("sampled", [False, True])
+@pytest.mark.parametrize("largest", [0.0, -5e5, 7.2e5, 7.3e5, 1e9, -3e38])
+def test_logits_far_from_zero(largest, sampled):
+    """The rows' largest logits on both sides of where the exponent's whole part is taken another way."""
+    c, rng = drafted(19, [4] * 4, 5000, dtype=torch.float32, sampled=sampled)
+    c["logits"] = c["logits"] * 60 + largest
+    c["logits"][:, ::3] = -3e38
+    c["logits"][:, 1::3][:, ::2] = -math.inf
+    check(run(**c), **c)
+
+
 def test_a_bad_row_in_the_middle_of_a_walk():
     V = 64
     logits = torch.zeros((3, V))
