@@ -36,7 +36,9 @@ constexpr double kLog2e = 1.4426950408889634074;
 // 2^y for y in [-2000, 0]: y = k + f with f in [-1/2, 1/2], 2^f by a polynomial of
 // degree 9 through the Chebyshev points of that interval (relative error below
 // 2e-14; 1 at f = 0).
-__device__ __forceinline__ double pow2_part(double f) {
+__device__ __forceinline__ double pow2(double y) {
+    const double k = __builtin_rint(y);
+    const double f = y - k;
     double p = 0x1.b6571de2f2351p-24;
     p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
     p = __builtin_fma(p, f, 0x1.ffcb76789860fp-17);
@@ -46,11 +48,8 @@ __device__ __forceinline__ double pow2_part(double f) {
     p = __builtin_fma(p, f, 0x1.c6b08d7044119p-5);
     p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
     p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
-    return __builtin_fma(p, f, 1.0);
-}
-__device__ __forceinline__ double pow2(double y) {
-    const double k = __builtin_rint(y);
-    return __builtin_ldexp(pow2_part(y - k), static_cast<int>(k));
+    p = __builtin_fma(p, f, 1.0);
+    return __builtin_ldexp(p, static_cast<int>(k));
 }
 
 // Weight of logit l <= m beside a finite maximum m; scale = log2(e) / T.  A logit
@@ -196,13 +195,13 @@ __device__ __forceinline__ double scale_of(float t) {
 }
 
 // ---------------------------------------------------------------------------
-// A wave holds its chunk's 2 048 logits in registers.  Bound by its instructions, 14
-// in fp64 and 3 others a logit: 432 rows of 131 072 bf16 logits take 39 us in steady
-// state (2.9 TB/s; 19 us without the weights).  Weights by their definition, 18 and 3
-// instructions, took 47 us where these take 42 (the first 60 launches).  Tried: a wave
-// that goes through many chunks with the next one's loads on their way (a fifth slower:
-// fewer waves fit), weights from a table of 2^(j/32) (no fewer instructions), exchanges
-// through LDS and a division in fp64 (a third slower).
+// A wave holds its chunk's 2 048 logits in registers.  Bound by its instructions, 9 in
+// fp64 and 5 others a logit and 150 a wave: 432 rows of 131 072 bf16 logits take 31 us
+// in steady state (3.6 TB/s; 19 us without the weights).  A polynomial of degree 9
+// without the table, 14 and 3 instructions: 39 us; weights by their definition, 18 and
+// 3: a tenth more than that.  Tried: a wave that goes through many chunks with the next
+// one's loads on their way (a fifth slower: fewer waves fit), exchanges through LDS and
+// a division in fp64 (a third slower).
 template <bool kF32>
 __global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) {
     const int lane = threadIdx.x & 63;
@@ -211,11 +210,21 @@ __global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) 
     if (blockIdx.x == 0 && node == 0 && threadIdx.x == 0) a.arrived[b] = 0;
     const NodeRange nodes = node_range(a.cu_nodes, b, a.num_nodes, a.max_nodes);
     const int chunks = logit_chunks(a.vocab);
-    if (node >= nodes.count || chunk >= chunks) return;
+    if (node >= nodes.count) return;
     const int64_t row = nodes.first + node;
     const float t = temperature_of(a, b);
     const int x0 = chunk * kLogitChunk + 8 * lane;
-    Round<Piece<kF32>> l = load_chunk<kF32>(a, row, chunk, x0);
+    Round<Piece<kF32>> l{};
+    if (chunk < chunks) l = load_chunk<kF32>(a, row, chunk, x0);
+    // 2^(j / 32), less j in the place where 32 k + j is added to its exponent (32 entries
+    // of 8 bytes: as many banks, so lanes with different ones don't meet)
+    __shared__ uint2 exponents[32];
+    if (threadIdx.x < 32) {
+        const uint64_t e = __builtin_bit_cast(uint64_t, pow2(lane * (1.0 / 32)));
+        exponents[lane] = make_uint2(static_cast<uint32_t>(e), static_cast<uint32_t>(e >> 32) - (static_cast<uint32_t>(lane) << 15));
+    }
+    __syncthreads();
+    if (chunk >= chunks) return;
     float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j)
@@ -237,21 +246,29 @@ __global__ __launch_bounds__(256, kF32 ? 5 : 8) void stats_kernel(VerifyArgs a) 
     } else if (m != -INFINITY) {
         const double scale = scale_of(t), top = m * scale;
         if (fabs(top) <= 0x1p20) {
-            // beside 2^K, K the whole number next to the maximum's exponent: then a logit's
-            // whole part k - K lies in the low bits of l scale + (1.5 2^52 - K), the rest is
-            // one exact product and difference away, and p 2^(k - K) joins the sum in one step.
-            // Logits below the maximum by 2^-140 or more weigh that (2^-129 of the sum for all).
-            const double whole = __builtin_rint(top), magic = 0x1.8p52 - whole;
+            // beside 2^K, K the whole number next to the maximum's exponent, in 32nds:
+            // l scale + (1.5 2^52 - 32 K) has a logit's number of 32nds in its low bits, 32 k
+            // + j, and the rest f in [-1/2, 1/2] is one exact product and difference away.
+            // 2^(f / 32) by a polynomial of degree 4 through the Chebyshev points (relative
+            // error below 2e-13, 1 at f = 0), times 2^(j / 32 + k) in the step that adds it.
+            // Logits below the maximum by 140 T or more weigh e^-140 (2^-190 of the sum for all).
+            const double whole = __builtin_rint(top), magic = 0x1.8p52 - 32.0 * whole, scale32 = 32.0 * scale;
             const float lowest = static_cast<float>(static_cast<double>(m) - 140.0 * static_cast<double>(t));
 #pragma unroll
             for (int j = 0; j < kSteps; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const double x = __builtin_elementwise_maximum(l.at[j][i], lowest);
-                    const double at = __builtin_fma(x, scale, magic);
-                    const double p = pow2_part(__builtin_fma(x, scale, magic - at));
-                    const uint32_t k = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, at));
-                    s = __builtin_fma(p, __builtin_bit_cast(double, static_cast<uint64_t>((k << 20) + 0x3FF00000u) << 32), s);
+                    const double at = __builtin_fma(x, scale32, magic);
+                    const double f = __builtin_fma(x, scale32, magic - at);
+                    const uint32_t n = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, at));
+                    const uint2 e = exponents[n % 32];
+                    double p = 0x1.3b2b07bdf358dp-27;
+                    p = __builtin_fma(p, f, 0x1.c6b13c3465457p-20);
+                    p = __builtin_fma(p, f, 0x1.ebfbdff82240ap-13);
+                    p = __builtin_fma(p, f, 0x1.62e42fef8dc67p-6);
+                    p = __builtin_fma(p, f, 1.0);
+                    s = __builtin_fma(p, __builtin_bit_cast(double, static_cast<uint64_t>((n << 15) + e.y) << 32 | e.x), s);
                 }
             s = wave_sum(s) * pow2(__builtin_fma(-static_cast<double>(m), scale, whole));
         } else {
