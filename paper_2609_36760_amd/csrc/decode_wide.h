@@ -638,6 +638,18 @@ __device__ __forceinline__ void clean_tile(uint8_t* tile, uint8_t* flags, int ti
 // are the last ones of a sequence; in them the hidden keys' scores are -inf, and
 // the tile is looked over first (clean_tile): a key with a channel that is not
 // finite would reach the rows that do not see it as 0 x NaN in the aggregation.
+
+// The sum of v over the lanes up to this one (of all 64).
+__device__ __forceinline__ int lanes_up_to(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // row_bcast 15
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // row_bcast 31
+    return v;
+}
+
 // What a workgroup of a tree launch works on.  The launch has as many as the plan's
 // splits would need if every sequence had the most rows; the ones that have work
 // come first.  Runs of them (tree_run) are dealt out to the XCDs (block id mod 8), so
@@ -649,7 +661,9 @@ __device__ __forceinline__ void clean_tile(uint8_t* tile, uint8_t* flags, int ti
 // has and that hold nothing.  Larger batches keep the sequences' order.
 // 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads: 510 us, 625 with splits
 // dealt out instead of row blocks, 632 so and in the sequences' order, 670 with
-// contiguous ranges of splits per XCD.
+// contiguous ranges of splits per XCD.  A workgroup finds its item in 1.4 us at 32
+// sequences (4.1 with sums by LDS shuffles and all kinds looked for: 8 nodes on 4K keys
+// at 16 heads 50.6 us, 48.4 so).
 struct TreeItem {
     int b, split, rb;
     int context;
@@ -676,7 +690,9 @@ __device__ __forceinline__ TreeItem tree_item(const TreeArgs& a, int lane) {
             }
             item.b = min(max(last, 0), a.B - 1);
             item.split = w - a.split_indptr[item.b];
-            item.alone = a.split_indptr[item.b + 1] - a.split_indptr[item.b] == 1;
+            const int planned = a.split_indptr[item.b + 1] - a.split_indptr[item.b];
+            item.alone = planned == 1;
+            item.some = item.split < planned;       // (the call may name more splits than the plan has)
         }
         item.context = a.seq_lens[item.b];
         return item;
@@ -691,33 +707,34 @@ __device__ __forceinline__ TreeItem tree_item(const TreeArgs& a, int lane) {
     const int count = min(max(planned, 0), a.num_work);
     const int whole = splits ? min(length / a.split_tokens, count) : 0;
     const int rest = count > whole ? length - whole * (splits ? a.split_tokens : 0) : -1;      // -1: no last split
-    // sums over the lanes before this one
-    auto before = [&](int v) {
-        int up = v;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(up, d);
-            up += lane >= d ? o : 0;
+    // The workgroups of a lane's whole splits, or last split, or empty splits: first one and
+    // number; only those of the kind that p lies in are looked for.
+    int n = whole * blocks, up = lanes_up_to(n), before = 0, kind = 0;
+    const int all0 = __builtin_amdgcn_readlane(up, 63);
+    if (p >= all0) {
+        const int n1 = rest >= 0 ? blocks : 0, up1 = lanes_up_to(n1), all1 = all0 + __builtin_amdgcn_readlane(up1, 63);
+        n = n1;
+        up = up1;
+        before = all0;
+        kind = 1;
+        if (p >= all1) {
+            n = max(count - whole - 1, 0) * blocks;
+            up = lanes_up_to(n);
+            before = all1;
+            kind = 2;
+        } else if (__builtin_amdgcn_ballot_w64(n1 > 0 && rest != __builtin_amdgcn_readfirstlane(rest)) != 0) {
+            up = n1;            // and of the last splits that are longer, or equal and before this lane's
+            for (int i = 0; i < a.B; ++i) {
+                const int other = __builtin_amdgcn_readlane(rest, i), of = __builtin_amdgcn_readlane(n1, i);
+                up += other > rest || (other == rest && i < lane) ? of : 0;
+            }
         }
-        return up - v;
-    };
-    // the workgroups of a lane's whole splits, last split and empty splits: first one and number
-    const int n0 = whole * blocks, n1 = rest >= 0 ? blocks : 0, n2 = max(count - whole - 1, 0) * blocks;
-    const int at0 = before(n0), all0 = __builtin_amdgcn_readlane(at0 + n0, 63);
-    int at1 = all0, all1 = all0;
-    for (int i = 0; i < a.B; ++i) {     // last splits that are longer, or equal and before this lane's
-        const int other = __builtin_amdgcn_readlane(rest, i), n = __builtin_amdgcn_readlane(n1, i);
-        at1 += other > rest || (other == rest && i < lane) ? n : 0;
-        all1 += n;
     }
-    const int at2 = all1 + before(n2);
-    const int in0 = p - at0, in1 = p - at1, in2 = p - at2;
-    const bool is0 = in0 >= 0 && in0 < n0, is1 = in1 >= 0 && in1 < n1, is2 = in2 >= 0 && in2 < n2;
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(is0 || is1 || is2);
+    const int in = p - before - (up - n);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(in >= 0 && in < n);
     TreeItem item{0, 0, 0, 0, 0, true, hit != 0};
     if (hit == 0) return item;
-    const int in = is0 ? in0 : is1 ? in1 : in2;
-    const int split = (is0 ? 0 : is1 ? whole : whole + 1) + (blocks > 0 ? in / blocks : 0);
+    const int split = (kind == 0 ? 0 : kind == 1 ? whole : whole + 1) + (blocks > 0 ? in / blocks : 0);
     const int rb = blocks > 0 ? in % blocks : 0;
     const int pick = __builtin_ctzll(hit);
     item.b = pick;

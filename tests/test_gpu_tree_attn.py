@@ -166,6 +166,19 @@ def test_more_sequences_than_lanes(kind, split, longer):
     b.check(split)
 
 
+@pytest.mark.parametrize("n", [3, 70])
+def test_more_splits_named_than_the_plan_has(n):
+    """A call captured for the most splits serves a plan of fewer: the last sequence has one split here."""
+    b = Batch(74, "c4", 16, [150] * (n - 1) + [20], trees(9, [4] * n), behind=1)
+    plan = b.plan(64)
+    plan["num_splits"] += 9
+    plan["workspace"] = torch.full((b.ms.mla_tree_workspace_bytes(plan["num_splits"], b.most, b.H),), 255, dtype=torch.uint8, device=DEV)
+    for _ in range(3):
+        b.out.fill_(-77.0)
+        b.call(**plan)
+        b.check(64)
+
+
 def test_as_many_sequences_as_lanes():
     rng = np.random.default_rng(1)
     b = Batch(72, "c4", 20, rng.integers(0, 300, 64).tolist(), trees(7, rng.integers(0, 9, 64).tolist()))
