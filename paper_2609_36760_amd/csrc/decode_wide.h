@@ -851,6 +851,11 @@ void decode_kernel(KernelArgs<kTree> a) {
     const int qi = row_ok ? row / a.H : 0;
     const int h = row_ok ? row % a.H : 0;
 
+    // the nodes it sees (loaded here: in the step of the tile that needs it, the wait for
+    // it is one for staging loads too; 24 ragged trees at 128 heads 498 us, 490 so)
+    [[maybe_unused]] uint64_t seen_nodes = 0;
+    if constexpr (kTree) seen_nodes = a.mask[node0 + qi];
+
     float m_ref = -INFINITY;    // reference of the exponentials (log2 units)
     float m_true = -INFINITY;   // true running maximum (log2 units)
     float l_run = 0.0f;         // this lane's share of the exponential sum
@@ -1070,6 +1075,7 @@ void decode_kernel(KernelArgs<kTree> a) {
         q_round(0);
         // the query rows are the youngest loads: every staged tile lands first
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if constexpr (kTree) asm volatile("" : "+v"(seen_nodes));
         q_read(0);
         if constexpr (kQRounds == 2) {
             // the second round overwrites the first's rows once they are read
@@ -1233,7 +1239,7 @@ void decode_kernel(KernelArgs<kTree> a) {
                 if (kTree && edge) {
                     if constexpr (kTree) {
                         const int first = kTS == 1 ? 4 * half : 16 * tw + 8 * half;     // of the lane's tokens
-                        const uint32_t seen = tree_bits(a.mask[node0 + qi], t0 - ctx, t_end - t0) >> first;
+                        const uint32_t seen = tree_bits(seen_nodes, t0 - ctx, t_end - t0) >> first;
                         const uint32_t bad = *reinterpret_cast<const uint32_t*>(smem + kFlags) >> first;
 #pragma unroll
                         for (int v = 0; v < kScores; ++v) {
