@@ -157,7 +157,7 @@ int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stri
  * rows are read before any of the sequence is written, so paths may be any.
  * Rows past the kept ones stay as they are.  new_lens[b] = ctx_lens[b] + keep[b].
  *   caches     device, [num_layers] pointers to caches of one format and size
- *              (256-byte aligned)
+ *              (256-byte aligned), none named twice
  *   path       device, int32 [B][max_nodes];  keep device, int32 [B]
  *   new_lens   device, int32 [B], another buffer than ctx_lens, or NULL
  * Entries outside [0, max_nodes), positions past the page table and page ids

@@ -192,8 +192,8 @@ def mla_verify_tree(logits, tokens, parents, cu_nodes, max_nodes, u_accept, u_dr
 
 
 class layer_caches:
-    """The caches of a model's layers (tensors of one size on one device) as the
-    table that the commit takes; keeps them alive."""
+    """The caches of a model's layers (tensors of one size on one device, each its
+    own memory) as the table that the commit takes; keeps them alive."""
 
     def __init__(self, tensors):
         _need(len(tensors) > 0, "layer_caches: at least one")
@@ -203,6 +203,8 @@ class layer_caches:
         _need(all(t.data_ptr() % 256 == 0 for t in tensors), "layer_caches: 256-byte aligned")
         self.tensors = list(tensors)
         self.bytes = size.pop()
+        at = sorted(t.data_ptr() for t in tensors)
+        _need(all(b - a >= max(self.bytes, 1) for a, b in zip(at, at[1:])), "layer_caches: each its own memory")
         self.table = torch.tensor([t.data_ptr() for t in tensors], dtype=I64, device=tensors[0].device)
 
 

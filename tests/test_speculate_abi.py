@@ -196,6 +196,10 @@ def test_binding_refuses_commit_tensors(ms, mb):
     at = -whole.data_ptr() % 256
     with pytest.raises(ValueError):
         ms.layer_caches([whole[at + 16:at + 4112]])
+    with pytest.raises(ValueError):         # a layer named twice would be moved twice, and layers may not overlap
+        ms.layer_caches([whole[at:at + 20736]] * 2)
+    with pytest.raises(ValueError):
+        ms.layer_caches([whole[at:at + 20736], whole[at + 256:at + 20992]])
     layers = ms.layer_caches([whole[at:at + 20736], whole[at + 20992:at + 41728]])
     assert layers.table.tolist() == [whole.data_ptr() + at, whole.data_ptr() + at + 20992]
     good = dict(layers=layers, num_pages=1, block_table=i32(2, 3), ctx_lens=i32(2), path=i32(2, 4), keep=i32(2), new_lens=i32(2))
