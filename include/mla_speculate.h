@@ -81,8 +81,11 @@ int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t 
  *   workspace  split only: at least mla_tree_workspace_bytes, 16-byte aligned
  * Rows of nodes from cu_nodes[B] on are neither read nor written.  Products and
  * weights as in the decode calls: fp16 operands over the low-bit cache, bf16
- * over the BF16 cache, fp32 sums, split partials in fp16; past the fp16 range
- * results are not finite.  A call repeats itself bit for bit.  B = 0 or
+ * over the BF16 cache, fp32 sums, split partials in fp16 (not finite past its
+ * range).  Scores of queries or context keys that are not finite, or past the
+ * fp16 range over the low-bit cache: NaN or +inf makes the row NaN (out and lse),
+ * split or not; a key of score -inf weighs nothing (0 times its values: NaN in a
+ * channel that is not finite).  A call repeats itself bit for bit.  B = 0 or
  * num_nodes = 0 is a no-op.
  */
 int mla_lowbit_tree_attn(const mla_cache_format* f, const uint16_t* q_lat, const uint16_t* q_rope,

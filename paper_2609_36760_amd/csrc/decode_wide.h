@@ -1617,7 +1617,9 @@ void decode_kernel(KernelArgs<kTree> a) {
     } else {
         const int64_t prow = (static_cast<int64_t>(w) * a.s_q + qi) * a.H + h;
         const float f = m_true == -INFINITY ? 0.0f : exp2f(m_ref - m_true);
-        a.part_m[prow] = m_true * kLn2;
+        // (a maximum leaves NaN out: under a tree a sum that is NaN takes +inf for it, so
+        // that the merge does not pass over a split whose scores are all NaN)
+        a.part_m[prow] = kTree && l_tot != l_tot ? INFINITY : m_true * kLn2;
         a.part_s[prow] = l_tot * f;
     }
 }
