@@ -699,8 +699,10 @@ __device__ __forceinline__ TreeItem tree_item(const TreeArgs& a, int lane) {
     }
     // this lane's sequence: its row blocks, splits, and whole splits
     const int b = min(lane, a.B - 1);
-    const int context = a.seq_lens[b], nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q).count;
-    const int length = max(context, 0) + nodes;
+    // (inside the page table first: any length of one sequence leaves the others' places alone)
+    const int context = min(max(a.seq_lens[b], 0), a.max_pages * a.g.page_size);
+    const int nodes = node_range(a.cu_nodes, b, a.num_nodes, a.s_q).count;
+    const int length = context + nodes;
     const int begin = splits ? a.split_indptr[b] : 0;
     const int planned = splits ? a.split_indptr[b + 1] - begin : 1;
     const int blocks = lane < a.B ? (nodes * a.H + kRows - 1) / kRows : 0;
