@@ -162,7 +162,7 @@ int mla_verify_tree(const void* logits, int32_t logits_type, int64_t logits_stri
  *   caches     device, [num_layers] pointers to caches of one format and size
  *              (256-byte aligned), none named twice
  *   path       device, int32 [B][max_nodes];  keep device, int32 [B]
- *   new_lens   device, int32 [B], another buffer than ctx_lens, or NULL
+ *   new_lens   device, int32 [B], or NULL; shares no memory with ctx_lens, path or keep
  * Entries outside [0, max_nodes), positions past the page table and page ids
  * outside the cache are passed over.  Sequences must own their pages from
  * position ctx_lens[b] on.  B = 0 or num_layers = 0 moves nothing.

@@ -218,6 +218,8 @@ def _commit(name, page_bytes, fmt, layers, num_pages, block_table, ctx_lens, pat
     _table(block_table, B)
     if new_lens is not None:
         _ints(new_lens, B, I32, "new_lens")
+        at = new_lens.data_ptr() - path.data_ptr()
+        _need(at <= -4 * B or at >= 4 * path.numel(), "new_lens: memory of its own")
     _on_device(layers.table, block_table, ctx_lens, path, keep, new_lens)
     mb._check(name, getattr(library(), name)(
         ctypes.byref(fmt), layers.table.data_ptr(), len(layers.tensors), num_pages, block_table.data_ptr(),

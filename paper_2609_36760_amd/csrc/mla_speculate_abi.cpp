@@ -34,6 +34,12 @@ int32_t rows_per_workgroup(int32_t max_nodes, int32_t H) {
     return static_cast<int64_t>(max_nodes) * H <= 64 ? 64 : mla::kDecodeRowsPerBlock;
 }
 
+// Whether n int32 at x and at y share memory.
+bool overlap(const int32_t* x, const int32_t* y, int64_t n) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y), size = 4 * static_cast<uintptr_t>(n);
+    return a < b ? b - a < size : a - b < size;
+}
+
 bool blocks_fit(int64_t blocks, int64_t threads) { return blocks * threads <= mla::kMaxDispatchItems; }
 
 // Estimated time of a call, us: its work items on the compute units in the order of
@@ -199,9 +205,11 @@ int commit(const mla_cache_format* f, bool lowbit, void* const* caches, int32_t 
     if (max_nodes > mla::kMaxNodes || B > kMaxGridAxis) return MLA_ENOTSUP;
     if (static_cast<int64_t>(max_pages_per_seq) * f->page_size > kMaxTokens) return MLA_ENOTSUP;
     if (B == 0 || (num_layers == 0 && new_lens == nullptr)) return MLA_OK;
-    if (ctx_lens == nullptr || path == nullptr || keep == nullptr || new_lens == ctx_lens) return MLA_EINVAL;
+    if (ctx_lens == nullptr || path == nullptr || keep == nullptr) return MLA_EINVAL;
     if (num_layers > 0 && (caches == nullptr || block_table == nullptr || num_pages == 0)) return MLA_EINVAL;
     if (!blocks_fit(static_cast<int64_t>(B) * std::max(num_layers, 1), 256)) return MLA_ENOTSUP;
+    // (a workgroup writes them while others still read the lengths and counts)
+    if (new_lens != nullptr && (overlap(new_lens, ctx_lens, B) || overlap(new_lens, keep, B))) return MLA_EINVAL;
     mla::CommitArgs a{};
     a.caches = reinterpret_cast<uint8_t* const*>(caches);
     a.num_layers = num_layers;
