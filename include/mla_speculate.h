@@ -124,10 +124,12 @@ int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab);
  * Tokens outside [0, vocab) are never taken.  Where r has no weight left (the
  * fixed drafts name every token of p, or the last token's share is lost to
  * rounding), the token is drawn from p.
- * Everything is computed in fp64 from the logits as they are (errors of the
- * weights below 1e-12, and of sums below 1e-12 of the row's whole sum), so that an
- * outcome differs from exact arithmetic's only where a random number lies that
- * close to a border.
+ * Everything is computed in fp64 from the logits as they are: errors of the
+ * weights below 1e-12 (of those above 1e-300), and of sums below 1e-12 of the row's
+ * whole sum, also of what rejections leave of it.  So an outcome differs from exact
+ * arithmetic's only where a random number lies within 1e-12 / s of a border, s the
+ * share of p that is left: 1 until a draft is rejected, and little after the
+ * rejection of a token with nearly all of p, or of one drawn from a q next to p.
  *   logits       device, fp32 or bf16 (logits_type) [num_nodes][logits_stride], first vocab used
  *   vocab        1 .. 2^21
  *   draft_probs  device, fp32 [num_nodes][draft_stride], first vocab used, or NULL

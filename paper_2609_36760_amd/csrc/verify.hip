@@ -593,7 +593,7 @@ __global__ __launch_bounds__(kWalk, 4) void walk_kernel(VerifyArgs a) {
                 cut = 0.0;
             }
             const double target = fmax(static_cast<double>(a.u_draw[b]), 0.0) * all;
-            // the first chunk that passes the target (for a number of 1, or NaN, the last with weight)
+            // the first chunk that passes the target (for a number of 1 the last with weight, for NaN as for 0)
             double at = up - sum;
             int first = kNone, final = -1;
 #pragma unroll
