@@ -112,9 +112,13 @@ int64_t mla_verify_workspace_bytes(int32_t num_nodes, int32_t B, int32_t vocab);
  *   fixed drafts (draft_probs NULL): r = p; for the node's children in their
  *     order, child i with token x is taken if u_accept[i] * sum(r) < r(x), else
  *     r(x) = 0;
- *   drawn drafts: child i was drawn from q, the draft_probs row of its parent;
+ *   drawn drafts: child i was drawn from q, the draft_probs row of its parent,
+ *     independently of the node's other children (a token may come twice);
  *     r = p; child i is taken if u_accept[i] * q(x) < r(x), else r becomes
- *     max(r - q, 0) over its sum (r stays if that sum is 0);
+ *     max(r - q, 0) over its sum (r stays if that sum is 0).  With children drawn
+ *     without replacement the emitted tokens would not be the target's: give those
+ *     as fixed drafts, which may be chosen in any way that does not look at the
+ *     random numbers;
  *   temperature 0, either way: a child is taken if its token is the largest
  *     logit's;
  * and with the child taken the walk goes on there.  With none taken the next

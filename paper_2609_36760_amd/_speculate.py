@@ -159,7 +159,8 @@ def mla_verify_tree(logits, tokens, parents, cu_nodes, max_nodes, u_accept, u_dr
     [nodes] and ``u_draw`` [B]: the nodes that stay into ``path`` [B, max_nodes],
     the emitted tokens into ``out_tokens``, their number into ``keep`` [B].
     ``draft_probs`` fp32 [nodes, vocab]: what every node's children were drawn
-    from (None: fixed drafts)."""
+    from, independently of each other (None: fixed drafts, those drawn without
+    replacement among them)."""
     _need(logits.dim() == 2, "logits: [nodes, vocab]")
     T, V = logits.shape
     B = u_draw.shape[0]
