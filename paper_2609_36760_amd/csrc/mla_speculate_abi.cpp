@@ -43,20 +43,21 @@ bool overlap(const int32_t* x, const int32_t* y, int64_t n) {
 bool blocks_fit(int64_t blocks, int64_t threads) { return blocks * threads <= mla::kMaxDispatchItems; }
 
 // Estimated time of a call, us: its work items on the compute units in the order of
-// the launch (whole splits, then the last ones of the sequences, the longest
-// first), and the merge.  `mixed`: 0, or sequences of an eighth to all of the rows,
-// which ones goes by the number.
+// the launch (up to 64 sequences whole splits, then the last ones of the sequences,
+// the longest first; past them sequence by sequence), and the merge.  `mixed`: 0, or
+// sequences of an eighth to all of the rows, which ones goes by the number.
 double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_wg, int64_t split_tokens, int mixed) {
     const double fixed = rows_wg == 64 ? 18.5 : 17.5, per_tile = rows_wg == 64 ? 1.25 : 1.6;
     const auto tiles = [](int64_t n) { return static_cast<double>((n + kTile - 1) / kTile); };
     struct Item { double time; int64_t blocks; };
     std::vector<Item> items, last;
+    const bool sorted = B <= mla::kWaveThreads;
     double partial_rows = 0.0;
     for (int32_t b = 0; b < B; ++b) {
         const int64_t own = mixed > 0 ? (rows * ((b * 5 + mixed) % 8 + 1) + 7) / 8 : rows, blocks = (own + rows_wg - 1) / rows_wg;
         const int64_t whole = seq_lens[b] / split_tokens, left = seq_lens[b] % split_tokens;
         if (whole > 0) items.push_back({fixed + per_tile * tiles(split_tokens), whole * blocks});
-        if (left > 0) last.push_back({fixed + per_tile * tiles(left), blocks});
+        if (left > 0) (sorted ? last : items).push_back({fixed + per_tile * tiles(left), blocks});
         if (seq_lens[b] > split_tokens) partial_rows += static_cast<double>(own * (whole + (left > 0 ? 1 : 0)));
     }
     std::sort(last.begin(), last.end(), [](const Item& x, const Item& y) { return x.time > y.time; });
