@@ -49,11 +49,16 @@ extern "C" {
  * Split size for mla_*_tree_attn over sequences of seq_lens tokens, drafted
  * ones included (host only; no HIP call): the multiple of 32 tokens, or 0
  * (unsplit), with the least estimated time of attention and merge.  The split
- * itself is mla_plan_splits's.
+ * itself is mla_plan_splits's, and any size gives right results.
  *   seq_lens  host, int32 [B], each >= 1
+ *   nodes     host, int32 [B], 0 .. max_nodes: of every sequence.  Without them
+ *             (mla_tree_split_tokens) sequences of one length are taken to have
+ *             max_nodes each, and in batches of several lengths an eighth of them
+ *             to all: up to half more time where ragged contexts have equal trees.
  * Returns it, or -MLA_EINVAL / -MLA_ENOTSUP.
  */
 int32_t mla_tree_split_tokens(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H);
+int32_t mla_tree_split_tokens_for(const int32_t* seq_lens, const int32_t* nodes, int32_t B, int32_t max_nodes, int32_t H);
 
 /* Bytes of the workspace of a split call; -1 for a negative or too large size. */
 int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t H);

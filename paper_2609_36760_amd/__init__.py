@@ -21,8 +21,8 @@ _PREFILL_NAMES = (
     "mla_prefill_attn", "rotation", "rms_norm", "MLA_ROPE_PAIRS", "MLA_ROPE_HALVES",
 )
 _SPECULATE_NAMES = (
-    "mla_tree_split_tokens", "mla_tree_workspace_bytes", "mla_lowbit_tree_attn", "mla_bf16_tree_attn",
-    "mla_verify_workspace_bytes", "mla_verify_tree", "layer_caches", "mla_lowbit_commit", "mla_bf16_commit",
+    "mla_tree_split_tokens", "mla_tree_split_tokens_for", "mla_tree_workspace_bytes", "mla_lowbit_tree_attn",
+    "mla_bf16_tree_attn", "mla_verify_workspace_bytes", "mla_verify_tree", "layer_caches", "mla_lowbit_commit", "mla_bf16_commit",
 )
 
 

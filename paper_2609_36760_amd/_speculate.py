@@ -16,7 +16,7 @@ from . import _binding as mb
 from ._prefill import BF16, D_C, D_R, F32, I32, I64, _cache, _int32s, _ints, _need, _on_device
 
 SYMBOLS = (
-    "mla_tree_split_tokens", "mla_tree_workspace_bytes", "mla_lowbit_tree_attn", "mla_bf16_tree_attn",
+    "mla_tree_split_tokens", "mla_tree_split_tokens_for", "mla_tree_workspace_bytes", "mla_lowbit_tree_attn", "mla_bf16_tree_attn",
     "mla_verify_workspace_bytes", "mla_verify_tree", "mla_lowbit_commit", "mla_bf16_commit",
 )
 
@@ -38,6 +38,7 @@ def library() -> ctypes.CDLL:
     commit = [P, P, I, L, P, I, P, P, P, I, I, P, P]
     sig = {
         "mla_tree_split_tokens": (I, [P, I, I, I]),
+        "mla_tree_split_tokens_for": (I, [P, P, I, I, I]),
         "mla_tree_workspace_bytes": (L, [I, I, I]),
         "mla_lowbit_tree_attn": (INT, attn),
         "mla_bf16_tree_attn": (INT, attn),
@@ -56,12 +57,23 @@ def library() -> ctypes.CDLL:
 
 def mla_tree_split_tokens(seq_lens, max_nodes: int, H: int) -> int:
     """Split size (0: unsplit) for sequences of ``seq_lens`` tokens, drafted
-    ones included; ``mla_plan_splits`` makes the plan."""
+    ones included, whose node counts are not known; ``mla_plan_splits`` makes
+    the plan."""
     lens = _int32s(seq_lens)
     _need(lens.ndim == 1, "seq_lens: one per sequence")
     n = library().mla_tree_split_tokens(lens.ctypes.data, lens.size, max_nodes, H)
     if n < 0:
         raise mb.MlaError("mla_tree_split_tokens", -n)
+    return n
+
+
+def mla_tree_split_tokens_for(seq_lens, nodes, max_nodes: int, H: int) -> int:
+    """The same for sequences of ``nodes`` drafted tokens."""
+    lens, counts = _int32s(seq_lens), _int32s(nodes)
+    _need(lens.ndim == 1 and counts.shape == lens.shape, "seq_lens, nodes: one per sequence")
+    n = library().mla_tree_split_tokens_for(lens.ctypes.data, counts.ctypes.data, lens.size, max_nodes, H)
+    if n < 0:
+        raise mb.MlaError("mla_tree_split_tokens_for", -n)
     return n
 
 

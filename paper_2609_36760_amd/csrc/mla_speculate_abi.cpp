@@ -44,17 +44,17 @@ bool blocks_fit(int64_t blocks, int64_t threads) { return blocks * threads <= ml
 
 // Estimated time of a call, us: its work items on the compute units in the order of
 // the launch (up to 64 sequences whole splits, then the last ones of the sequences,
-// the longest first; past them sequence by sequence), and the merge.  `mixed`: 0, or
-// sequences of an eighth to all of the rows, which ones goes by the number.
-double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_wg, int64_t split_tokens, int mixed) {
+// the longest first; past them sequence by sequence), and the merge.  rows: of every
+// sequence.  The costs are those of low-bit caches.
+double tree_cost(const int32_t* seq_lens, const std::vector<int64_t>& rows, int32_t rows_wg, int64_t split_tokens) {
     const double fixed = rows_wg == 64 ? 18.5 : 17.5, per_tile = rows_wg == 64 ? 1.25 : 1.6;
     const auto tiles = [](int64_t n) { return static_cast<double>((n + kTile - 1) / kTile); };
     struct Item { double time; int64_t blocks; };
     std::vector<Item> items, last;
-    const bool sorted = B <= mla::kWaveThreads;
+    const bool sorted = rows.size() <= mla::kWaveThreads;
     double partial_rows = 0.0;
-    for (int32_t b = 0; b < B; ++b) {
-        const int64_t own = mixed > 0 ? (rows * ((b * 5 + mixed) % 8 + 1) + 7) / 8 : rows, blocks = (own + rows_wg - 1) / rows_wg;
+    for (size_t b = 0; b < rows.size(); ++b) {
+        const int64_t own = rows[b], blocks = (own + rows_wg - 1) / rows_wg;
         const int64_t whole = seq_lens[b] / split_tokens, left = seq_lens[b] % split_tokens;
         if (whole > 0) items.push_back({fixed + per_tile * tiles(split_tokens), whole * blocks});
         if (left > 0) (sorted ? last : items).push_back({fixed + per_tile * tiles(left), blocks});
@@ -76,7 +76,8 @@ double tree_cost(const int32_t* seq_lens, int32_t B, int64_t rows, int32_t rows_
     return partial_rows == 0.0 ? longest : longest + 4.0 + 2.0 * partial_rows * kPartialBytes / 4e6;
 }
 
-int32_t split_size(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H) {
+// nodes: of every sequence, or NULL where they are not known.
+int32_t split_size(const int32_t* seq_lens, const int32_t* nodes, int32_t B, int32_t max_nodes, int32_t H) {
     int64_t tokens = 0;
     int32_t longest = 0;
     for (int32_t b = 0; b < B; ++b) {
@@ -85,33 +86,55 @@ int32_t split_size(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_
     }
     if (B == 0) return 0;
     const int32_t rows_wg = rows_per_workgroup(max_nodes, H);
-    // How many nodes the sequences have is not known here.  Sequences of one length are
-    // taken to have the most, others to be a mixed batch, for which the estimate says
-    // little about single sizes: there the smallest size within 4 % of the best one is
-    // taken, whose items end closer together.
-    bool mixed = false;
-    for (int32_t b = 1; b < B; ++b) mixed = mixed || seq_lens[b] != seq_lens[0];
-    const int64_t rows = static_cast<int64_t>(max_nodes) * H, row_blocks = (rows + rows_wg - 1) / rows_wg;
-    // unsplit, sizes of about a quarter more each time, and even parts of the longest
-    // sequence, as long as there are not far more workgroups than compute units
+    const int64_t most = static_cast<int64_t>(max_nodes) * H, row_blocks = (most + rows_wg - 1) / rows_wg;
     constexpr int64_t kMostBlocks = 16 * mla::kCus;
     if (B * row_blocks >= kMostBlocks) return 0;
+    // Without the nodes, sequences of one length are taken to have the most, others to be
+    // a mixed batch: three guesses at who has an eighth to all of the rows, which say
+    // little about single sizes, so that the smallest size within 4 % of the best one is
+    // taken, whose items end closer together.  Ragged contexts behind equal trees pay for
+    // that (128 heads: 8 x 4 nodes 107 us with their nodes given, 156 without; 24 x 4
+    // 202, 231; 64 x 4 553, 636; 24 x 13 at 64 heads of one length but for a token 165,
+    // 202), ragged ones behind ragged trees little (32 sequences of up to 8: 235, 255; 24
+    // of up to 32: 676, 651).
+    bool mixed = false;
+    for (int32_t b = 1; b < B && nodes == nullptr; ++b) mixed = mixed || seq_lens[b] != seq_lens[0];
+    std::vector<std::vector<int64_t>> guesses(mixed ? 3 : 1, std::vector<int64_t>(static_cast<size_t>(B)));
+    for (size_t k = 0; k < guesses.size(); ++k)
+        for (int32_t b = 0; b < B; ++b) {
+            const int64_t eighths = mixed ? (int64_t{b} * 5 + 3 * static_cast<int64_t>(k) + 1) % 8 + 1 : 8;
+            guesses[k][static_cast<size_t>(b)] = nodes != nullptr ? static_cast<int64_t>(nodes[b]) * H : (most * eighths + 7) / 8;
+        }
+    // unsplit, sizes of about a quarter more each time, and even parts of the longest
+    // sequence, as long as there are not far more workgroups than compute units
     std::vector<int64_t> sizes{(int64_t{longest} + kTile - 1) / kTile * kTile};
     for (int64_t s = kTile; s < longest; s = (s + std::max<int64_t>(s / 4, 1) + kTile - 1) / kTile * kTile) sizes.push_back(s);
     for (int64_t parts = 2; parts <= 32; ++parts) sizes.push_back((longest + parts * kTile - 1) / (parts * kTile) * kTile);
     std::vector<double> times;
     for (size_t i = 0; i < sizes.size(); ++i) {
         const bool no = i > 0 && (sizes[i] >= longest || (tokens / sizes[i] + B) * row_blocks > kMostBlocks);
-        double time = 0.0;
-        for (int k = mixed ? 1 : 0; !no && k < (mixed ? 8 : 1); k += 3)
-            time += tree_cost(seq_lens, B, rows, rows_wg, sizes[i], k);
-        times.push_back(no ? HUGE_VAL : time);
+        double time = no ? HUGE_VAL : 0.0;
+        for (size_t k = 0; !no && k < guesses.size(); ++k) time += tree_cost(seq_lens, guesses[k], rows_wg, sizes[i]);
+        times.push_back(time);
     }
     const double best = *std::min_element(times.begin(), times.end());
+    if (best == 0.0) return 0;          // no nodes at all
     size_t pick = sizes.size();
     for (size_t i = 0; i < sizes.size(); ++i)
         if (times[i] <= (mixed ? 1.04 : 1.0) * best && (pick == sizes.size() || sizes[i] < sizes[pick])) pick = i;
     return pick == 0 ? 0 : static_cast<int32_t>(sizes[pick]);
+}
+
+int32_t checked_split_size(const int32_t* seq_lens, const int32_t* nodes, int32_t B, int32_t max_nodes, int32_t H) {
+    if (B < 0 || max_nodes < 1 || H < 1 || (B > 0 && seq_lens == nullptr)) return -MLA_EINVAL;
+    if (!sizes_ok(max_nodes, H)) return -MLA_ENOTSUP;
+    for (int32_t b = 0; b < B; ++b)
+        if (seq_lens[b] < 1 || (nodes != nullptr && (nodes[b] < 0 || nodes[b] > max_nodes))) return -MLA_EINVAL;
+    try {
+        return split_size(seq_lens, nodes, B, max_nodes, H);
+    } catch (const std::exception&) {       // no memory for the estimate: any size is a right one
+        return 0;
+    }
 }
 
 int tree_attn(const mla_cache_format* f, bool lowbit, const uint16_t* q_lat, const uint16_t* q_rope,
@@ -232,15 +255,12 @@ int commit(const mla_cache_format* f, bool lowbit, void* const* caches, int32_t 
 extern "C" {
 
 int32_t mla_tree_split_tokens(const int32_t* seq_lens, int32_t B, int32_t max_nodes, int32_t H) {
-    if (B < 0 || max_nodes < 1 || H < 1 || (B > 0 && seq_lens == nullptr)) return -MLA_EINVAL;
-    if (!sizes_ok(max_nodes, H)) return -MLA_ENOTSUP;
-    for (int32_t b = 0; b < B; ++b)
-        if (seq_lens[b] < 1) return -MLA_EINVAL;
-    try {
-        return split_size(seq_lens, B, max_nodes, H);
-    } catch (const std::exception&) {       // no memory for the estimate: any size is a right one
-        return 0;
-    }
+    return checked_split_size(seq_lens, nullptr, B, max_nodes, H);
+}
+
+int32_t mla_tree_split_tokens_for(const int32_t* seq_lens, const int32_t* nodes, int32_t B, int32_t max_nodes, int32_t H) {
+    if (B > 0 && nodes == nullptr) return -MLA_EINVAL;
+    return checked_split_size(seq_lens, nodes, B, max_nodes, H);
 }
 
 int64_t mla_tree_workspace_bytes(int32_t num_splits, int32_t max_nodes, int32_t H) {
