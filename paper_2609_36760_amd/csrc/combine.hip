@@ -172,8 +172,9 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(std::conditional_t
 // Rows of a tree launch.  Where a batch is ragged most rows that the sizes allow do
 // not exist, or need no merge; as many waves as the card holds go through those that
 // do, found by the lanes' sequences (up to 64 of them; larger batches go through
-// all rows).  24 sequences of up to 32 nodes at 128 heads: 19 us, 35 with a wave for
-// every row that may exist (bound by being started), 35 with one for every eight.
+// all rows).  24 sequences of up to 32 nodes at 128 heads, all of them merged: 19 us, 35
+// with a wave for every row that may exist (bound by being started), 35 with one for
+// every eight; 11.6 where those of one split write their rows themselves, as now.
 template <int kBatch>
 __global__ __launch_bounds__(64 * kWaves) void tree_rows_kernel(TreeCombineArgs a) {
     const int rows_per_seq = a.s_q * a.H;

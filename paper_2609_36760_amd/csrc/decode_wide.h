@@ -659,9 +659,9 @@ __device__ __forceinline__ int lanes_up_to(int v) {
 // sequences (one per lane) the whole splits of all sequences come first, then
 // their last ones, the longest first, then those that a plan for longer sequences
 // has and that hold nothing.  Larger batches keep the sequences' order.
-// 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads: 510 us, 625 with splits
-// dealt out instead of row blocks, 632 so and in the sequences' order, 670 with
-// contiguous ranges of splits per XCD.  A workgroup finds its item in 1.4 us at 32
+// 24 sequences of 1K-16K tokens and 5-32 nodes at 128 heads, the call when this was
+// chosen (501 us now): 510 us, 625 with splits dealt out instead of row blocks, 632 so
+// and in the sequences' order, 670 with contiguous ranges of splits per XCD.  A workgroup finds its item in 1.4 us at 32
 // sequences (4.1 with sums by LDS shuffles and all kinds looked for: 8 nodes on 4K keys
 // at 16 heads 50.6 us, 48.4 so).
 struct TreeItem {
